@@ -235,6 +235,109 @@ pc_status pc_backward(pc_circuit *c, const float *theta, const float *tables, co
 pc_status pc_em_step(pc_circuit *c, float *theta, float *tables, float *theta_flow, float *table_flow,
                      float step, float pseudocount, void *stream);
 
+/* ---- Token models over circuits: predicting a variable, distilling from a teacher, decoding with beams ----
+ * None of these calls needs a handle: their operands are what the descriptors name, which is read before the call
+ * returns and not retained.  They run on the device the calling thread has current.  Like the passes they only
+ * enqueue kernels on `stream` and may be captured; a call with no rows (groups) does nothing and returns PC_OK.
+ * Workspaces are scratch of one call: nothing in them is kept from call to call, calls that overlap in time need
+ * one each. */
+enum { PC_F32 = 0, PC_BF16 = 1, PC_F16 = 2 };   /* element types of rows of logits */
+
+/* Input nodes of one variable with their weights in each sample: n_blocks blocks of K nodes; block j's weights are the rows
+ * rows[j] .. rows[j] + K - 1 of `weights` (samples contiguous, `stride` floats between rows, stride >= B), its categorical
+ * table is tables[table[j]].  rows / table are device arrays of n_blocks entries, or NULL: rows[j] = j * K, table[j] = j.  A
+ * block whose rows or table lie outside [0, n_rows) / [0, n_tables) is left out.  The weights are not negative. */
+typedef struct {
+    int32_t K, n_blocks, n_cats, n_tables;
+    int64_t n_rows, stride;
+    const float *weights;
+    const int32_t *rows, *table;
+} pc_mixture;
+
+/* The input blocks of variable `var` with their node flows F in a workspace that pc_backward has just filled (same
+ * workspace and B as that call, else PC_ERR_STATE).  Where the variable is marginalised the flows are the probabilities of
+ * its input nodes given the sample's evidence, so that pc_predict answers p(x_var | evidence).  (In a sample that observes
+ * the variable they are the probabilities given that value too.)  Pointers stay valid until the workspace's next pass. */
+pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void *workspace, size_t workspace_bytes,
+                         pc_mixture *out);
+
+/* Predictive distribution:  logp[b][c] = log sum_j sum_k weights[rows[j] + k][b] * tables[table[j]][c][k],  b < B, c < n_cats,
+ * ld >= n_cats floats between the rows of logp.  A probability below FLT_MIN (a sample without weights: all of them) gives
+ * -inf. */
+pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *stream);
+
+/* Its flows for a gradient dlogp of an objective with respect to logp, the weights held fixed (the responsibilities of an
+ * EM step):
+ *   flow[t][c][k] = tables[t][c][k] * sum over b and the blocks j of table t of weights[rows[j] + k][b] * dlogp[b][c] / exp(logp[b][c]),
+ * which is the objective's gradient with respect to log tables[t][c][k];  table_flow = scale * flow for the tables that the mixture
+ * names, added to what is there where `accumulate` is set.  With dlogp = -q (a loss -sum q logp, q >= 0) and scale = -1 these are
+ * the flows of an EM step on soft targets, ready for pc_em_step.  Entries of logp below log FLT_MIN add nothing. */
+pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t B, const float *logp, int64_t logp_ld,
+                              const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow, void *stream);
+
+/* Distillation from a teacher's top logits.  Per row, with temperature T:
+ *   q_j  = softmax over the listed entries of teacher_j / T, or exp(teacher_j / T - teacher_lse) where the teacher's own
+ *          log-normaliser (at T) over its whole vocabulary is given
+ *   logp = log-softmax of student / T over its n_cats entries, or the row itself where `normalised` (log-probabilities, T = 1)
+ *   loss = sum_j q_j (log q_j - logp[ids_j]);   dloss / dstudent_c = (p_c sum_j q_j - sum_{j: ids_j = c} q_j) / T,
+ * without the p_c term where `normalised` (then -gradient is the soft target of pc_predict_backward).
+ * ids outside [0, n_cats) are no entries (padding of short lists: -1), as are teacher logits of -inf; a category listed twice counts
+ * twice.  A row without entries has loss 0 and gradient 0 whatever the student's row holds.  A student logit of -inf has p = 0;
+ * loss is +inf where such a category, or any in a row of nothing else, is listed with q > 0.  NaN and +inf in a row make its
+ * results NaN (a `normalised` row: only where they are listed). */
+#define PC_MAX_TOP 1024
+typedef struct {
+    int64_t rows;
+    int32_t n_cats, top;                         /* entries of a student row; of a teacher's list, 1 .. PC_MAX_TOP */
+    const void *student;  int32_t student_type;  int64_t student_ld;     /* ld: elements between rows              */
+    const int32_t *ids;                          int64_t ids_ld;
+    const void *teacher;  int32_t teacher_type;  int64_t teacher_ld;
+    const float *teacher_lse;                    /* [rows] or NULL                                                  */
+    float temperature;                           /* > 0                                                             */
+    int32_t normalised;
+} pc_distill;
+pc_status pc_distill_workspace_bytes(const pc_distill *d, size_t *bytes);
+/* loss: device fp32 [rows]; stats: device fp32 [rows][2], the row's maximum m and log sum exp((student - m) / T) (zeros where
+ * `normalised`), for pc_distill_backward.  workspace: 16-byte aligned. */
+pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t workspace_bytes, float *loss, float *stats, void *stream);
+/* dstudent[r][c] = scale * dloss[r] * gradient, rounded once to the student's type; dloss: device fp32 [rows] or NULL (ones);
+ * dstudent_ld >= n_cats elements between rows; dstudent may be the student's rows themselves (same ld).  Rows whose scale * dloss is 0
+ * get 0 whatever they hold. */
+pc_status pc_distill_backward(const pc_distill *d, const float *stats, const float *dloss, float scale, void *dstudent,
+                              int64_t dstudent_ld, void *stream);
+
+/* Beam search: of all beams and categories of a group the n_out best.  Candidate (beam, c) has the score
+ * running[beam] + z, z = scores[beam][c], minus log sum_c' exp(scores[beam][c']) where `normalise` (rows of logits), taken in 64 bits.
+ * A finished beam (done != 0) has the one candidate done_token with z = 0; its row is not read.  Order: higher score, then lower
+ * beam, then (within a beam) higher z, then lower category.  Candidates that are no numbers or whose beam's running score is
+ * no number below +inf count as -inf, as do all of a row whose log-normaliser is no finite number; candidates of -inf come last, by
+ * beam and category.  So a group's output is complete and the same on every run. */
+#define PC_MAX_BEAMS 64
+#define PC_MAX_BEAM_OUT 64
+typedef struct {
+    int32_t groups, beams, n_cats, n_out;        /* beams 1 .. PC_MAX_BEAMS; n_out 1 .. PC_MAX_BEAM_OUT, at most beams * n_cats */
+    const void *scores;  int32_t scores_type;  int64_t scores_ld;        /* [groups * beams][ld]                  */
+    int32_t normalise;
+    const float *running;                        /* [groups][beams] or NULL (zeros)                               */
+    const uint8_t *done;                         /* [groups][beams] or NULL                                       */
+    int32_t done_token;
+} pc_beam;
+pc_status pc_beam_workspace_bytes(const pc_beam *a, size_t *bytes);
+/* out_scores (fp32), parents (beam within the group), tokens: device, [groups][n_out], best first.  workspace: 16-byte aligned. */
+pc_status pc_beam_select(const pc_beam *a, void *workspace, size_t workspace_bytes, float *out_scores, int32_t *parents,
+                         int32_t *tokens, void *stream);
+/* What each survivor takes along: row g * n_out + i of dst = row g * beams + parents[g][i] of src, for up to PC_MAX_STATES arrays
+ * of rows in one launch (evidence rows x and mask, hidden states, caches).  Strides are in bytes; a row's bytes behind row_bytes
+ * are not touched.  dst must not overlap any src or other dst (PC_ERR_ARG).  A parent outside [0, beams) leaves its row of dst as it was. */
+#define PC_MAX_STATES 16
+typedef struct {
+    const void *src;
+    void *dst;
+    int64_t row_bytes, src_stride, dst_stride;
+} pc_state;
+pc_status pc_beam_reorder(const pc_state *states, int32_t n_states, const int32_t *parents, int32_t groups, int32_t beams,
+                          int32_t n_out, void *stream);
+
 /* Per-kernel timing for benchmarks (the measurement protocol, not an operation of the paper).  While enabled,
  * every kernel launch of forward / backward / EM is bracketed by two HIP events on the launch stream.
  * pc_profile_read waits for the recorded events (it synchronises with the work launched so far) and returns

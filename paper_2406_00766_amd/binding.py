@@ -61,11 +61,36 @@ class pc_profile(C.Structure):
                 ("bf16_launches", C.c_int64 * 16)]
 
 
+class pc_mixture(C.Structure):
+    _fields_ = [("K", C.c_int32), ("n_blocks", C.c_int32), ("n_cats", C.c_int32), ("n_tables", C.c_int32),
+                ("n_rows", C.c_int64), ("stride", C.c_int64), ("weights", C.c_void_p), ("rows", C.c_void_p), ("table", C.c_void_p)]
+
+
+class pc_distill(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n_cats", C.c_int32), ("top", C.c_int32),
+                ("student", C.c_void_p), ("student_type", C.c_int32), ("student_ld", C.c_int64),
+                ("ids", C.c_void_p), ("ids_ld", C.c_int64),
+                ("teacher", C.c_void_p), ("teacher_type", C.c_int32), ("teacher_ld", C.c_int64),
+                ("teacher_lse", C.c_void_p), ("temperature", C.c_float), ("normalised", C.c_int32)]
+
+
+class pc_beam(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("beams", C.c_int32), ("n_cats", C.c_int32), ("n_out", C.c_int32),
+                ("scores", C.c_void_p), ("scores_type", C.c_int32), ("scores_ld", C.c_int64), ("normalise", C.c_int32),
+                ("running", C.c_void_p), ("done", C.c_void_p), ("done_token", C.c_int32)]
+
+
+class pc_state(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("row_bytes", C.c_int64), ("src_stride", C.c_int64), ("dst_stride", C.c_int64)]
+
+
 EXPORTS = ["pc_compile", "pc_compile_host", "pc_destroy", "pc_last_error", "pc_get_sizes", "pc_get_layer",
            "pc_get_group", "pc_copy_group", "pc_get_kernel", "pc_workspace_layout", "pc_workspace_bytes", "pc_forward",
            "pc_forward_static", "pc_backward", "pc_em_step", "pc_profile_enable", "pc_profile_read", "pc_kernel_class_name",
            "pc_measure_copy", "pc_measure_mfma_f32", "pc_collapse", "pc_collapsed_dag", "pc_collapsed_theta",
-           "pc_collapsed_block_map", "pc_collapsed_destroy", "pc_order_for_scratch", "pc_set_wait_limit"]
+           "pc_collapsed_block_map", "pc_collapsed_destroy", "pc_order_for_scratch", "pc_set_wait_limit",
+           "pc_get_mixture", "pc_predict", "pc_predict_backward", "pc_distill_workspace_bytes", "pc_distill_forward",
+           "pc_distill_backward", "pc_beam_workspace_bytes", "pc_beam_select", "pc_beam_reorder"]
 
 _lib = None
 
@@ -115,6 +140,16 @@ def lib():
         L.pc_collapsed_block_map.restype = C.POINTER(C.c_int32)
         L.pc_collapsed_destroy.argtypes = [C.c_void_p]
         L.pc_collapsed_destroy.restype = None
+        L.pc_get_mixture.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(pc_mixture)]
+        L.pc_predict.argtypes = [C.POINTER(pc_mixture), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        L.pc_predict_backward.argtypes = [C.POINTER(pc_mixture), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                          C.c_float, C.c_int32, C.c_void_p, C.c_void_p]
+        L.pc_distill_workspace_bytes.argtypes = [C.POINTER(pc_distill), C.POINTER(C.c_size_t)]
+        L.pc_distill_forward.argtypes = [C.POINTER(pc_distill), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.pc_distill_backward.argtypes = [C.POINTER(pc_distill), C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
+        L.pc_beam_workspace_bytes.argtypes = [C.POINTER(pc_beam), C.POINTER(C.c_size_t)]
+        L.pc_beam_select.argtypes = [C.POINTER(pc_beam), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.pc_beam_reorder.argtypes = [C.POINTER(pc_state), C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
         _lib = L
     return _lib
 
@@ -331,6 +366,220 @@ def pc_measure_mfma_f32(out_buf, out_bytes: int, reps: int = 5, stream=None) -> 
     return float(out.value)
 
 
+# ---- token models over circuits: these take torch tensors, whose shapes, types and strides become the descriptors ----
+def _refuse(message: str):
+    raise PcError(1, message)
+
+
+def _tensor(name, t, dtype=None, shape=None, device=None, last=1):
+    """Check one argument: a tensor on the GPU (on `device`), of this type and shape (None: any length), its last `last` axes
+    contiguous.  The kernels trust what is passed on from here."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        _refuse(f"{name} must be a tensor")
+    if t.device.type != "cuda" or (device is not None and t.device != device):
+        _refuse(f"{name} must lie on {device if device is not None else 'a GPU'}, not on {t.device}")
+    if dtype is not None and t.dtype != dtype:
+        _refuse(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
+        _refuse(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+    step = 1
+    for n, st in list(zip(t.shape, t.stride()))[::-1][:last]:
+        if n > 1 and st != step:
+            _refuse(f"the last {last} axes of {name} must be contiguous")
+        step *= n
+    return t
+
+
+def _ld(t):
+    """Elements between the rows of a matrix (its length where there is but one row, whose stride means nothing)."""
+    n = t.shape[1]
+    if t.shape[0] > 1 and t.stride(0) < n:
+        _refuse("the rows of a matrix must not overlap")
+    return t.stride(0) if t.shape[0] > 1 else n
+
+
+def _type(name, t):
+    import torch
+    types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # PC_F32, PC_BF16, PC_F16
+    if t.dtype not in types:
+        _refuse(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
+    return types[t.dtype]
+
+
+def _call(device, stream, function, *args):
+    """function(*args, stream) with `device` current; stream None: that device's current stream."""
+    import torch
+    if device.index is None or device.index == torch.cuda.current_device():
+        _check(function(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(function(*args, _stream(stream)))
+
+
+class mixture:
+    """pc_mixture over tensors: weights float32 [n_rows, >= B], samples contiguous; block j is rows rows[j] .. + K and table
+    table[j] (int32 tensors), or rows j * K .. and table j.  `n_tables` defaults to n_blocks."""
+
+    def __init__(self, weights, K, n_cats, n_blocks, rows=None, table=None, n_tables=None):
+        import torch
+        _tensor("weights", weights, torch.float32, (None, None))
+        self.device, self.columns = weights.device, int(weights.shape[1])
+        for name, t in (("rows", rows), ("table", table)):
+            if t is not None:
+                _tensor(name, t, torch.int32, (n_blocks,), self.device)
+        self.keep = (weights, rows, table)
+        self.struct = pc_mixture(int(K), int(n_blocks), int(n_cats), int(n_blocks if n_tables is None else n_tables), int(weights.shape[0]),
+                                 _ld(weights), weights.data_ptr(), _ptr(rows), _ptr(table))
+
+
+def pc_get_mixture(handle, var, B, workspace, workspace_bytes) -> mixture:
+    """The input blocks of variable `var` with the node flows that pc_backward has left in the workspace (a tensor)."""
+    m = mixture.__new__(mixture)
+    m.struct = pc_mixture()
+    _check(lib().pc_get_mixture(handle, int(var), int(B), _ptr(workspace), int(workspace_bytes), C.byref(m.struct)))
+    m.device, m.columns, m.keep = workspace.device, int(m.struct.stride), (workspace,)
+    return m
+
+
+def _check_predict(m, tables, B, name, out):
+    import torch
+    s = m.struct
+    _tensor("tables", tables, torch.float32, None, m.device, tables.dim() if isinstance(tables, torch.Tensor) else 1)
+    if tables.numel() != s.n_tables * s.n_cats * s.K:
+        _refuse(f"tables must hold {s.n_tables} x {s.n_cats} x {s.K} floats")
+    if B > m.columns:
+        _refuse("weights have fewer than B columns")
+    _tensor(name, out, torch.float32, (B, s.n_cats), m.device)
+
+
+def pc_predict(m: mixture, tables, B, logp, stream=None):
+    """logp float32 [B, n_cats] (rows may be strided) = log sum of weights * tables."""
+    _check_predict(m, tables, B, "logp", logp)
+    _call(m.device, stream, lib().pc_predict, C.byref(m.struct), tables.data_ptr(), int(B), logp.data_ptr(), _ld(logp))
+
+
+def pc_predict_backward(m: mixture, tables, B, logp, dlogp, scale, table_flow, accumulate=True, stream=None):
+    """Table flows for a gradient dlogp [B, n_cats] of an objective; added to table_flow, or stored."""
+    import torch
+    _check_predict(m, tables, B, "logp", logp)
+    _tensor("dlogp", dlogp, torch.float32, (B, m.struct.n_cats), m.device)
+    _tensor("table_flow", table_flow, torch.float32, None, m.device, table_flow.dim() if isinstance(table_flow, torch.Tensor) else 1)
+    if table_flow.numel() != tables.numel():
+        _refuse("table_flow must be as long as tables")
+    _call(m.device, stream, lib().pc_predict_backward, C.byref(m.struct), tables.data_ptr(), int(B), logp.data_ptr(), _ld(logp),
+          dlogp.data_ptr(), _ld(dlogp), float(scale), int(bool(accumulate)), table_flow.data_ptr())
+
+
+class distill:
+    """pc_distill over tensors: student [rows, n_cats], ids int32 [rows, top], teacher [rows, top], teacher_lse float32 [rows]."""
+
+    def __init__(self, student, ids, teacher, temperature=1.0, teacher_lse=None, normalised=False):
+        import torch
+        _tensor("student", student, None, (None, None))
+        self.device = student.device
+        rows = int(student.shape[0])
+        _tensor("ids", ids, torch.int32, (rows, None), self.device)
+        _tensor("teacher", teacher, None, (rows, ids.shape[1]), self.device)
+        if teacher_lse is not None:
+            _tensor("teacher_lse", teacher_lse, torch.float32, (rows,), self.device)
+        self.keep = (student, ids, teacher, teacher_lse)
+        self.student = student
+        self.struct = pc_distill(rows, int(student.shape[1]), int(ids.shape[1]), student.data_ptr(), _type("student", student), _ld(student),
+                                 ids.data_ptr(), _ld(ids), teacher.data_ptr(), _type("teacher", teacher), _ld(teacher),
+                                 _ptr(teacher_lse), float(temperature), int(bool(normalised)))
+
+
+def pc_distill_workspace_bytes(d: distill) -> int:
+    n = C.c_size_t()
+    _check(lib().pc_distill_workspace_bytes(C.byref(d.struct), C.byref(n)))
+    return int(n.value)
+
+
+def _workspace(t, device):
+    import torch
+    if t is None:
+        return None, 0
+    _tensor("workspace", t, torch.uint8, (None,), device)
+    return t.data_ptr(), t.numel()
+
+
+def pc_distill_forward(d: distill, workspace, loss, stats, stream=None):
+    """loss float32 [rows], stats float32 [rows, 2]."""
+    import torch
+    _tensor("loss", loss, torch.float32, (d.struct.rows,), d.device)
+    _tensor("stats", stats, torch.float32, (d.struct.rows, 2), d.device, 2)
+    _call(d.device, stream, lib().pc_distill_forward, C.byref(d.struct), *_workspace(workspace, d.device), loss.data_ptr(), stats.data_ptr())
+
+
+def pc_distill_backward(d: distill, stats, dloss, scale, dstudent, stream=None):
+    """dstudent [rows, n_cats] of the student's type = scale * dloss (float32 [rows] or None) * gradient; it may be the student itself."""
+    import torch
+    _tensor("stats", stats, torch.float32, (d.struct.rows, 2), d.device, 2)
+    if dloss is not None:
+        _tensor("dloss", dloss, torch.float32, (d.struct.rows,), d.device)
+    _tensor("dstudent", dstudent, d.student.dtype, tuple(d.student.shape), d.device)
+    _call(d.device, stream, lib().pc_distill_backward, C.byref(d.struct), stats.data_ptr(), _ptr(dloss), float(scale), dstudent.data_ptr(), _ld(dstudent))
+
+
+class beam:
+    """pc_beam over tensors: scores [groups * beams, n_cats], running float32 [groups, beams], done uint8 [groups, beams]."""
+
+    def __init__(self, scores, running, n_out, done=None, done_token=0, normalise=False):
+        import torch
+        _tensor("scores", scores, None, (None, None))
+        self.device = scores.device
+        _tensor("running", running, torch.float32, (None, None), self.device, 2)
+        groups, beams = int(running.shape[0]), int(running.shape[1])
+        if scores.shape[0] != groups * beams:
+            _refuse("scores must have a row for each running score")
+        if done is not None:
+            _tensor("done", done, torch.uint8, (groups, beams), self.device, 2)
+        self.keep = (scores, running, done)
+        self.struct = pc_beam(groups, beams, int(scores.shape[1]), int(n_out), scores.data_ptr(), _type("scores", scores), _ld(scores),
+                              int(bool(normalise)), running.data_ptr(), _ptr(done), int(done_token))
+
+
+def pc_beam_workspace_bytes(a: beam) -> int:
+    n = C.c_size_t()
+    _check(lib().pc_beam_workspace_bytes(C.byref(a.struct), C.byref(n)))
+    return int(n.value)
+
+
+def pc_beam_select(a: beam, workspace, out_scores, parents, tokens, stream=None):
+    """The n_out best of each group: out_scores float32, parents int32 and tokens int32, all [groups, n_out]."""
+    import torch
+    shape = (a.struct.groups, a.struct.n_out)
+    for name, t, dtype in (("out_scores", out_scores, torch.float32), ("parents", parents, torch.int32), ("tokens", tokens, torch.int32)):
+        _tensor(name, t, dtype, shape, a.device, 2)
+    _call(a.device, stream, lib().pc_beam_select, C.byref(a.struct), *_workspace(workspace, a.device), out_scores.data_ptr(),
+          parents.data_ptr(), tokens.data_ptr())
+
+
+def pc_beam_reorder(states, parents, beams, stream=None):
+    """For each (src, dst) of `states`: row g * n_out + i of dst = row g * beams + parents[g, i] of src.  Rows are the leading axis;
+    a row's elements are contiguous, rows may be strided."""
+    import torch
+    _tensor("parents", parents, torch.int32, (None, None), None, 2)
+    groups, n_out, beams = int(parents.shape[0]), int(parents.shape[1]), int(beams)
+    if not 1 <= len(states) <= 16:
+        _refuse("1 .. 16 states")
+    array = (pc_state * len(states))()
+    for s, (src, dst) in zip(array, states):
+        for name, t, rows in (("src", src, groups * beams), ("dst", dst, groups * n_out)):
+            _tensor(name, t, None, None, parents.device, max(1, t.dim() - 1) if isinstance(t, torch.Tensor) else 1)
+            if t.dim() < 1 or t.shape[0] != rows:
+                _refuse(f"{name} must have {rows} rows")
+        if src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
+            _refuse("src and dst must have rows of one shape and type")
+        n = src[:1].numel() if src.shape[0] else 1
+        e = src.element_size()
+        s.src, s.dst, s.row_bytes = src.data_ptr(), dst.data_ptr(), n * e
+        s.src_stride = src.stride(0) * e if src.shape[0] > 1 else n * e
+        s.dst_stride = dst.stride(0) * e if dst.shape[0] > 1 else n * e
+    _call(parents.device, stream, lib().pc_beam_reorder, array, len(states), parents.data_ptr(), groups, beams, n_out)
+
+
 def compiled_tables(handle: int) -> list[dict]:
     """All layers with their groups copied to host: [{kind, depth, fwd: [(ids, nbr, par)], bwd: [...]}]."""
     out = []
@@ -394,6 +643,19 @@ class Circuit:
 
     def em_step(self, step=1.0, pseudocount=0.0):
         pc_em_step(self.handle, self.theta, self.tables, self.theta_flow, self.table_flow, step, pseudocount)
+
+    def predict(self, var, logp=None):
+        """log p(x_var = c | the batch's evidence) [B, n_cats], after backward() on a batch in which `var` is marginalised."""
+        m = pc_get_mixture(self.handle, var, self.B, self._ws, self._ws.numel())
+        if logp is None:
+            logp = self.torch.empty((self.B, self.sizes.n_cats), dtype=self.torch.float32, device=self.device)
+        pc_predict(m, self.tables, self.B, logp)
+        return logp
+
+    def predict_backward(self, var, logp, dlogp, scale=1.0):
+        """Adds the table flows of a gradient with respect to predict(var) to table_flow."""
+        m = pc_get_mixture(self.handle, var, self.B, self._ws, self._ws.numel())
+        pc_predict_backward(m, self.tables, self.B, logp, dlogp, scale, self.table_flow)
 
     def node_buffers(self):
         """(l, F, R) float32 views of the workspace: l, F are [n_rows, stride] (row = compiled node offset),

@@ -125,6 +125,7 @@ pc_status upload(pc_circuit *c, hipStream_t stream)
     add(&c->d_em_seg_ptr, c->em_seg_ptr); add(&c->d_em_seg, c->em_seg);
     add(&c->d_init_ids, c->init_ids);
     add(&c->d_flow_rep, c->flow_rep);
+    add(&c->d_mix_rows, c->mix_rows); add(&c->d_mix_tabs, c->mix_tabs);
     add(&c->d_pf_pb, c->pf_pb); add(&c->d_pf_ptr, c->pf_ptr); add(&c->d_pf_sum, c->pf_sum); add(&c->d_pf_child, c->pf_child);
     for (ChainTab *t : {&c->chain_fwd, &c->chain_bwd}) add(&t->d_words, t->words);
     for (FlowTab *f : {&c->flow_fwd, &c->flow_bwd}) { add(&f->d_ent, f->ent); add(&f->d_rec, f->rec); add(&f->d_list, f->list); }
@@ -521,6 +522,7 @@ static pc_status forward_on(pc_circuit *c, const float *theta, const float *tabl
     int32_t *xT = (int32_t *)(base + w.xt_off);
     const int32_t K = c->K;
     c->fw_B = -1;
+    if (c->bw_workspace == workspace) c->bw_B = -1;
 
     const size_t L = c->layers.size(), li0 = flow_start(c, w, false);
     FlowDev flow{};
@@ -699,6 +701,28 @@ pc_status pc_backward(pc_circuit *c, const float *theta, const float *tables, co
         launch_param_flow(theta, l, R, N, nfmax, theta_flow, pf, K, w.Bs, s);
     }
     PC_HIP(hipGetLastError());
+    c->bw_workspace = workspace;
+    c->bw_B = B;
+    return PC_OK;
+}
+
+pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void *workspace, size_t workspace_bytes, pc_mixture *out)
+{
+    if (!c || !workspace || !out) return fail(PC_ERR_ARG, "NULL argument");
+    if (!c->on_device) return fail(PC_ERR_STATE, "circuit was compiled without a device");
+    if (var < 0 || var >= c->n_vars) return fail(PC_ERR_ARG, "var out of range");
+    if (B < 1) return fail(PC_ERR_ARG, "B must be positive");
+    if (c->bw_workspace != workspace || c->bw_B != B)
+        return fail(PC_ERR_STATE, "pc_get_mixture needs the pc_backward that just ran on the same workspace and B");
+    const Ws w = ws_layout(c, B);
+    if (workspace_bytes < w.total) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_workspace_bytes");
+    if (check_fault(c) != PC_OK) return PC_ERR_HIP;
+    const int32_t first = c->mix_ptr[var], n = c->mix_ptr[var + 1] - first;
+    if (n == 0) return fail(PC_ERR_ARG, "no input block reads this variable");
+    out->K = c->K; out->n_blocks = n; out->n_cats = c->n_cats; out->n_tables = c->n_tables;
+    out->n_rows = w.l_rows; out->stride = w.Bs;
+    out->weights = (const float *)((const char *)workspace + w.f_off);
+    out->rows = c->d_mix_rows + first; out->table = c->d_mix_tabs + first;
     return PC_OK;
 }
 
@@ -717,7 +741,7 @@ pc_status pc_em_step(pc_circuit *c, float *theta, float *tables, float *theta_fl
              c->d_pb_cols, c->d_group_nch, c->d_em_seg_ptr, c->d_em_seg, c->d_em_part, c->d_ztab};
     launch_em(theta, tables, theta_flow, table_flow, em, c->K, c->n_tables, c->n_cats, step, pseudocount, (hipStream_t)stream);
     PC_HIP(hipGetLastError());
-    c->fw_B = -1;
+    c->fw_B = c->bw_B = -1;
     return PC_OK;
 }
 

@@ -16,6 +16,7 @@
 #include <limits>
 #include <map>
 #include <numeric>
+#include <tuple>
 #include <unordered_map>
 
 #include "pc_internal.h"
@@ -720,6 +721,17 @@ pc_status compile_host(const pc_dag *d, pc_circuit *c, bool tables_on_host)
             std::vector<int32_t> tabs = g.par;                          // a table shared by several blocks: flows collide
             std::sort(tabs.begin(), tabs.end());
             g.tied_in_group = std::adjacent_find(tabs.begin(), tabs.end()) != tabs.end();
+            std::vector<int32_t> order(blocks);                          // blocks by variable, table, offset
+            std::sort(order.begin(), order.end(), [&](int32_t a, int32_t b) {
+                return std::make_tuple(d->in_var[a], d->in_table[a], a) < std::make_tuple(d->in_var[b], d->in_table[b], b);
+            });
+            c->mix_ptr.assign((size_t)d->n_vars + 1, 0);
+            for (int32_t u : order) {
+                ++c->mix_ptr[d->in_var[u] + 1];
+                c->mix_rows.push_back((u + 1) * K);
+                c->mix_tabs.push_back(d->in_table[u]);
+            }
+            for (int32_t v = 0; v < d->n_vars; ++v) c->mix_ptr[v + 1] += c->mix_ptr[v];
             layer.fwd.push_back(std::move(g));
         } else if (tables_on_host) {
             std::vector<Row> fwd_rows;

@@ -128,6 +128,10 @@ struct pc_circuit {
     std::vector<int32_t> flow_rep;
     int32_t *d_flow_rep = nullptr;
 
+    // input blocks by variable (CSR over mix_rows: node offsets, mix_tabs: tables; within a variable by table, then offset)
+    std::vector<int32_t> mix_ptr, mix_rows, mix_tabs;
+    int32_t *d_mix_rows = nullptr, *d_mix_tabs = nullptr;
+
     // dataflow launches (empty where they do not apply)
     pc::FlowTab flow_fwd, flow_bwd;
     pc::ChainTab chain_fwd, chain_bwd;
@@ -165,6 +169,9 @@ struct pc_circuit {
     const void *fw_workspace = nullptr;
     const void *fw_theta = nullptr, *fw_tables = nullptr, *fw_x = nullptr, *fw_mask = nullptr;
     int32_t fw_B = -1;
+    // the workspace that holds the node flows of the last pc_backward, for pc_get_mixture
+    const void *bw_workspace = nullptr;
+    int32_t bw_B = -1;
 };
 
 namespace pc {

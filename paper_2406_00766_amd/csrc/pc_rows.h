@@ -1,0 +1,52 @@
+// Rows of logits in several element types, and the launch checks that the calls on them share (internal).
+#pragma once
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <string>
+
+#include "pc_internal.h"
+
+namespace pc {
+
+#define PC_LOG2E_F 1.4426950408889634f
+#define PC_NEG_INF_F (-__builtin_inff())
+
+struct bf16_t { uint16_t bits; };                     // bfloat16 as it lies in memory
+typedef __half f16_t;
+
+__device__ inline float to_f32(float v) { return v; }
+__device__ inline float to_f32(bf16_t v) { return __uint_as_float((uint32_t)v.bits << 16); }
+__device__ inline float to_f32(f16_t v) { return __half2float(v); }
+// to nearest, ties to even; a NaN stays one
+template <typename T> __device__ T from_f32(float v);
+template <> __device__ inline float from_f32<float>(float v) { return v; }
+template <> __device__ inline f16_t from_f32<f16_t>(float v) { return __float2half_rn(v); }
+template <> __device__ inline bf16_t from_f32<bf16_t>(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    return bf16_t{(uint16_t)(v != v ? (u >> 16) | 0x40 : (u + 0x7fff + ((u >> 16) & 1)) >> 16)};
+}
+
+inline int64_t type_bytes(int32_t type) { return type == PC_F32 ? 4 : 2; }
+inline bool type_known(int32_t type) { return type == PC_F32 || type == PC_BF16 || type == PC_F16; }
+inline bool aligned_to(const void *p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+
+// f(element) for the C++ type of `type`
+template <typename F>
+inline void with_type(int32_t type, F f)
+{
+    if (type == PC_F32) f(float{});
+    else if (type == PC_BF16) f(bf16_t{});
+    else f(f16_t{});
+}
+
+inline pc_status launched()
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PC_OK : fail(PC_ERR_HIP, std::string("launch: ") + hipGetErrorString(e));
+}
+
+}  // namespace pc

@@ -1,0 +1,215 @@
+"""pc_predict / pc_predict_backward against the same sums in 64 bits: any block size, block lists with gaps, repeated tables and entries out
+of range, batches on both sides of the tile sizes, samples of probability 0, strided rows; the flows against differences of the
+objective; conditionals of whole circuits against the oracle's forward pass.
+
+Tolerances.  A product of two fp32 operands taken as bf16 pairs (hi + lo, each rounded by at most 2^-8 relative) loses at most
+3 * 2^-16 of itself (either operand's remainder, lo * lo); fp32 accumulation of n non-negative terms at most n * 2^-24 of
+the sum.  A probability is so off by the factor e = 3 * 2^-16 + H * 2^-24, its logarithm by e absolutely, and the stored
+logarithm by 2^-23 relative more (logf, rounding).  A flow is a sum over samples of W * (g / p) in fp32 operands that are kept to 2^-23 each:
+its error is at most (n + 32) * 2^-24 of the sum of the terms' absolute values (n terms; exp(-logp) is good to a few 2^-24 since
+|logp| < 88 is given exactly and the argument's reduction is exact to 2^-24 of the result's exponent)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import pc_oracle as orc
+from paper_2406_00766_amd import binding as pcb
+from paper_2406_00766_amd import workloads as W
+from tests.replay import replayed
+
+pytestmark = pytest.mark.gpu
+FLT_MIN = float(np.finfo(np.float32).tiny)
+
+
+def make(K, n_blocks, V, B, seed, extra_cols=0, empty=(), zero_share=0.0):
+    """Weights [H, B + extra] whose columns add up to one (NaN behind the last sample), tables [n_blocks, V, K] of distributions."""
+    rng = np.random.default_rng(seed)
+    w = rng.exponential(size=(K * n_blocks, B)) ** 3
+    w[rng.random(w.shape) < zero_share] = 0.0
+    w /= np.maximum(w.sum(0, keepdims=True), 1e-30)
+    w[:, list(empty)] = 0.0
+    full = np.full((K * n_blocks, B + extra_cols), np.nan, dtype=np.float32)
+    full[:, :B] = w
+    t = rng.exponential(size=(n_blocks, V, K)) ** 2
+    t /= t.sum(1, keepdims=True)
+    return full, t.astype(np.float32)
+
+
+def exact_p(full, t, B, rows, table):
+    K = t.shape[2]
+    p = np.zeros((B, t.shape[1]))
+    for r, j in zip(rows, table):
+        if 0 <= r <= full.shape[0] - K and 0 <= j < t.shape[0]:
+            p += full[r:r + K, :B].astype(np.float64).T @ t[j].astype(np.float64).T
+    return p
+
+
+def check_logp(got, p, H):
+    want = np.where(p >= FLT_MIN, np.log(np.maximum(p, FLT_MIN)), -np.inf)
+    edge = np.abs(p / FLT_MIN - 1) < 1e-3                  # next to the cut either answer is right
+    fin = np.isfinite(want) & ~edge
+    assert np.array_equal(np.isneginf(got) | edge, np.isneginf(want) | edge)
+    tol = 3 * 2.0 ** -16 + H * 2.0 ** -24 + np.abs(want[fin]) * 2.0 ** -23
+    worst = np.max(np.abs(got[fin] - want[fin]) / tol) if fin.any() else 0.0
+    assert worst <= 1.0, worst
+
+
+def check_flow(got, want, bound, n):
+    """bound: the sum of the terms' absolute values."""
+    tol = (n + 32) * 2.0 ** -24 * bound + FLT_MIN
+    worst = np.max(np.abs(got - want) / tol)
+    assert worst <= 1.0, worst
+
+
+SIZES = [(1, 1, 1, 1), (1, 3, 2, 5), (2, 1, 7, 33), (7, 5, 65, 31), (16, 1, 64, 32), (16, 3, 129, 64), (24, 2, 31, 65), (32, 1, 300, 1),
+         (32, 9, 33, 130), (33, 2, 70, 20), (48, 2, 260, 3), (64, 2, 256, 257), (64, 7, 1000, 77), (96, 1, 63, 128), (100, 3, 65, 16),
+         (127, 1, 127, 127), (128, 3, 517, 40), (128, 2, 5003, 1), (128, 1, 32, 513), (64, 1, 4099, 300)]
+
+
+@pytest.mark.parametrize("K,nb,V,B", SIZES)
+def test_predict_and_flows_match_64_bits(K, nb, V, B):
+    print(f"case predict K={K} blocks={nb} V={V} B={B}", flush=True)
+    full, t = make(K, nb, V, B, K + V + B, extra_cols=B % 3, empty=(B // 2,) if B > 2 else (), zero_share=0.3)
+    w, tables = torch.from_numpy(full).cuda(), torch.from_numpy(t).cuda()
+    m = pcb.mixture(w, K, V, nb)
+    pad = V % 5
+    out = torch.full((B, V + pad), 7.0, device="cuda")
+    pcb.pc_predict(m, tables, B, out[:, :V])
+    p = exact_p(full, t, B, np.arange(nb) * K, range(nb))
+    got = out.cpu().numpy()
+    assert np.all(got[:, V:] == 7.0)
+    check_logp(got[:, :V].astype(np.float64), p, K * nb)
+    # flows: a signed gradient, zeros among it
+    rng = np.random.default_rng(5)
+    g = (rng.normal(size=(B, V)) * (rng.random((B, V)) < 0.7)).astype(np.float32)
+    logp = got[:, :V].copy()
+    r = np.where(np.isneginf(logp), 0.0, g * np.exp(-np.where(np.isneginf(logp), 0.0, logp).astype(np.float64)))
+    f64 = np.where(np.isnan(full[:, :B]), 0, full[:, :B]).astype(np.float64)
+    sums = (f64 @ r).reshape(nb, K, V).transpose(0, 2, 1) * t
+    bound = (f64 @ np.abs(r)).reshape(nb, K, V).transpose(0, 2, 1) * t
+    base = rng.random(t.shape).astype(np.float32)
+    for accumulate in (False, True):
+        flow = torch.from_numpy(base.copy()).cuda()
+        pcb.pc_predict_backward(m, tables, B, out[:, :V], torch.from_numpy(g).cuda(), -0.5, flow, accumulate=accumulate)
+        want = -0.5 * sums + (base if accumulate else 0.0)
+        check_flow(flow.cpu().numpy().astype(np.float64), want, 0.5 * bound + (base if accumulate else 0.0), B)
+
+
+def test_block_lists_with_gaps_shared_tables_and_entries_out_of_range():
+    K, V, B = 32, 90, 45
+    full, t = make(K, 8, V, B, 3)
+    rows = np.array([32, 128, 5, 250, -32, 64, 64, 96], dtype=np.int32)          # 250 + 32 > 256 and -32 are outside
+    table = np.array([2, 0, 2, 1, 1, 7, 8, 2], dtype=np.int32)                  # 8 is outside; 2 is used by three blocks
+    w, tables = torch.from_numpy(full).cuda(), torch.from_numpy(t).cuda()
+    m = pcb.mixture(w, K, V, 8, rows=torch.from_numpy(rows).cuda(), table=torch.from_numpy(table).cuda(), n_tables=8)
+    out = torch.empty((B, V), device="cuda")
+    pcb.pc_predict(m, tables, B, out)
+    check_logp(out.cpu().numpy().astype(np.float64), exact_p(full, t, B, rows, table), 8 * K)
+    g = np.random.default_rng(1).normal(size=(B, V)).astype(np.float32)
+    flow = torch.full(t.shape, 3.0, device="cuda")
+    pcb.pc_predict_backward(m, tables, B, out, torch.from_numpy(g).cuda(), 1.0, flow, accumulate=False)
+    got = flow.cpu().numpy().astype(np.float64)
+    r = g / np.exp(out.cpu().numpy().astype(np.float64))
+    for j in range(8):
+        mine = [a for a, b in zip(rows, table) if b == j and 0 <= a <= 224]
+        if not mine:
+            assert np.all(got[j] == 3.0)                   # a table that no block names is not touched
+            continue
+        ws = sum(full[a:a + K].astype(np.float64) for a in mine)
+        check_flow(got[j], (ws @ r).T * t[j], (ws @ np.abs(r)).T * t[j], B * len(mine))
+
+
+def test_flows_are_the_gradient_with_respect_to_log_tables():
+    """Differences of the objective in 64 bits: O(eps^2) = 1e-8 of the second derivative, relative."""
+    K, nb, V, B = 16, 2, 9, 11
+    full, t = make(K, nb, V, B, 8)
+    g = np.random.default_rng(2).normal(size=(B, V)).astype(np.float32)
+    m = pcb.mixture(torch.from_numpy(full).cuda(), K, V, nb)
+    tables, out, flow = torch.from_numpy(t).cuda(), torch.empty((B, V), device="cuda"), torch.zeros(t.shape, device="cuda")
+    pcb.pc_predict(m, tables, B, out)
+    pcb.pc_predict_backward(m, tables, B, out, torch.from_numpy(g).cuda(), 1.0, flow)
+    got, eps = flow.cpu().numpy(), 1e-4
+    objective = lambda tt: float(np.sum(g * np.log(exact_p(full, tt, B, np.arange(nb) * K, range(nb)))))
+    for at in [(0, 0, 0), (1, 8, 15), (0, 4, 7), (1, 2, 3)]:
+        up, down = t.astype(np.float64), t.astype(np.float64)
+        up[at] *= np.exp(eps)
+        down[at] *= np.exp(-eps)
+        assert abs((objective(up) - objective(down)) / (2 * eps) - got[at]) <= 1e-5 * np.sum(np.abs(g))
+
+
+@pytest.mark.parametrize("make_w", [lambda: W.hmm(5, 64, 30, 32, 21, 3), lambda: W.hclt(9, 64, 64, 40, 9, n_cats=17),
+                                    lambda: W.rat_spn(16, 2, 2, 32, 16, 33, 4, n_cats=11), lambda: W.hmm(4, 12, 9, 4, 7, 11)])
+def test_conditionals_of_circuits_match_the_oracle(make_w):
+    """p(x_v = c | rest) = p(x_v = c, rest) / p(rest), both from the oracle: the flows behind it carry the path's own
+    tolerance (1e-3 relative)."""
+    w = make_w()
+    c = pcb.Circuit(w)
+    v = w.n_vars - 1
+    mask = (np.random.default_rng(4).random(w.x.shape) < 0.3).astype(np.uint8)
+    mask[:, v] = 1
+    c.set_batch(w.x, mask)
+    c.forward()
+    with pytest.raises(pcb.PcError) as e:
+        c.predict(v)
+    assert e.value.status_name == "PC_ERR_STATE"           # no flows yet
+    c.backward(theta_flow=False, table_flow=False)
+    print(f"case conditional {w.name}", flush=True)
+    got = np.exp(c.predict(v).double().cpu().numpy())
+    rest = orc.forward(w, w.theta, w.tables, w.x, mask)[1]
+    seen = mask.copy()
+    seen[:, v] = 0
+    for cat in range(w.n_cats):
+        x = w.x.copy()
+        x[:, v] = cat
+        want = np.exp(orc.forward(w.with_batch(x), w.theta, w.tables, x, seen)[1] - rest)
+        assert np.all(np.abs(got[:, cat] - want) <= 1e-3 * want + 1e-7), cat
+    assert np.all(np.abs(got.sum(1) - 1) <= 1e-3)
+    c.em_step()
+    with pytest.raises(pcb.PcError) as e:
+        c.predict(v)                                       # the parameters are others now
+    assert e.value.status_name == "PC_ERR_STATE"
+    c.close()
+
+
+def test_predictions_in_product_scratch_mode_and_of_a_sample_of_probability_0():
+    w = W.hmm(4, 64, 30, 32, 9, 3)
+    c, cs = pcb.Circuit(w), pcb.Circuit(pcb.pc_order_for_scratch(w))
+    mask = np.zeros(w.x.shape, np.uint8)
+    mask[:, 2] = 1
+    x = w.x.copy()
+    x[4, 0] = -5                                           # outside the support
+    out = []
+    for k in (c, cs):
+        k.set_batch(x, mask)
+        k.forward()
+        k.backward()
+        out.append(k.predict(2).cpu().numpy())
+    assert np.all(np.isneginf(out[0][4])) and np.all(np.isneginf(out[1][4]))
+    keep = np.arange(9) != 4
+    assert np.all(np.isfinite(out[0][keep])) and np.all(np.abs(out[0][keep] - out[1][keep]) <= 1e-4)
+    g = torch.ones((9, 30), device="cuda")
+    c.table_flow.zero_()
+    c.predict_backward(2, torch.from_numpy(out[0]).cuda(), g)
+    assert bool(torch.isfinite(c.table_flow).all())
+    assert abs(float(c.table_flow.sum()) - 8 * 30) <= 1e-3 * 240     # sum over states of T W / p is 1 per sample and category
+    c.close(); cs.close()
+
+
+def test_predict_captured_and_replayed_on_changing_inputs():
+    K, nb, V, B = 64, 3, 333, 50
+    full, t = make(K, nb, V, B, 12)
+    w, tables = torch.from_numpy(full).cuda(), torch.from_numpy(t).cuda()
+    m = pcb.mixture(w, K, V, nb)
+    out, flow, g = torch.empty((B, V), device="cuda"), torch.zeros(t.shape, device="cuda"), torch.randn((B, V), device="cuda")
+
+    def step():
+        pcb.pc_predict(m, tables, B, out)
+        pcb.pc_predict_backward(m, tables, B, out, g, 1.0, flow, accumulate=False)
+        return out, flow
+
+    def change():
+        w.copy_(torch.roll(w, 1, 1))
+        g.neg_()
+
+    replayed(step, change)
