@@ -43,107 +43,329 @@ __device__ inline float running_score(const BeamDev &a, int64_t row)
     return v < __builtin_inff() ? v : PC_NEG_INF_F;
 }
 
-// The n best of each row as keys (best first; 0: none), and its log-normaliser.  One workgroup a row, one pass per survivor.
-template <typename T>
-__global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, uint64_t *__restrict__ best, double *__restrict__ lse)
+// ---- sorting across the lanes of a wave, best first ----
+// Candidates of different beams: score, then lower `place` (beam, then rank within the beam).
+struct Cand {
+    double score;
+    uint32_t place;
+    int32_t token;
+};
+constexpr uint32_t kNoPlace = ~0u;
+__device__ inline float lane_xor(float v, int j) { return __shfl_xor(v, j); }
+__device__ inline uint64_t lane_xor(uint64_t v, int j) { return __shfl_xor((unsigned long long)v, j); }
+__device__ inline Cand lane_xor(const Cand &v, int j) { return Cand{__shfl_xor(v.score, j), (uint32_t)__shfl_xor((int)v.place, j), __shfl_xor(v.token, j)}; }
+__device__ inline bool better(float a, float b) { return a > b; }
+__device__ inline bool better(uint64_t a, uint64_t b) { return a > b; }
+__device__ inline bool better(const Cand &a, const Cand &b) { return a.score > b.score || (a.score == b.score && a.place < b.place); }
+// One step: of a lane and its partner j away the better stays in the one chosen by `first`.
+template <typename V>
+__device__ inline V exchange(const V &v, int j, bool first)
 {
-    __shared__ uint64_t top[kBeamThreads / 64];
-    __shared__ double part[kBeamThreads / 64];
-    const int64_t rows = (int64_t)a.groups * a.beams;
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T *z = (const T *)a.scores + r * a.ld;
-        const bool done = a.done && a.done[r], dead = running_score(a, r) == PC_NEG_INF_F;
-        double norm = 0.0;
-        uint64_t last = ~0ull;
-        for (int n = 0; n < a.n_out; ++n) {
-            uint64_t mine = 0;
-            if (!done && !dead)
-                for (int c = threadIdx.x; c < a.n_cats; c += kBeamThreads) {
-                    const uint64_t k = candidate(to_f32(z[c]), c);
-                    if (k < last && k > mine) mine = k;
-                }
-            for (int d = 32; d > 0; d >>= 1) mine = max(mine, (uint64_t)__shfl_xor((unsigned long long)mine, d));
-            __syncthreads();
-            if (threadIdx.x % 64 == 0) top[threadIdx.x / 64] = mine;
-            __syncthreads();
-            for (int w = 0; w < kBeamThreads / 64; ++w) mine = max(mine, top[w]);
-            if (n == 0 && a.normalise && !done && !dead) {
-                const float m = key_value((uint32_t)(mine >> 32));
-                double s = 0.0;
-                for (int c = threadIdx.x; c < a.n_cats; c += kBeamThreads) s += (double)expf(to_f32(z[c]) - m);
-                for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
-                if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
-                __syncthreads();
-                s = 0.0;
-                for (int w = 0; w < kBeamThreads / 64; ++w) s += part[w];
-                norm = (double)m + log(s);
-            }
-            if (threadIdx.x == 0) best[r * a.n_out + n] = mine;
-            last = mine;
+    const V o = lane_xor(v, j);
+    return better(o, v) == first ? o : v;              // keys are distinct, or equal in all that counts
+}
+template <typename V>
+__device__ inline V sort_lanes(V v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 2; k <= 64; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j > 0; j >>= 1) v = exchange(v, j, ((lane & j) == 0) == ((lane & k) == 0));
+    return v;
+}
+// The 64 best of two sorted lists; `other` holds the second one in reverse (lane i: its entry 63 - i).
+template <typename V>
+__device__ inline V merge_lanes(const V &v, const V &other)
+{
+    const int lane = threadIdx.x & 63;
+    V r = better(other, v) ? other : v;
+#pragma unroll
+    for (int j = 32; j > 0; j >>= 1) r = exchange(r, j, (lane & j) == 0);
+    return r;
+}
+// n-th largest (n <= 64) of one value per thread.  No NaN.
+__device__ inline float block_nth(float v, int n, float (&lds)[kBeamThreads])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    v = sort_lanes(v);
+    __syncthreads();
+    lds[threadIdx.x] = v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 1; w < kBeamThreads / 64; ++w) v = merge_lanes(v, lds[(wave + w) % (kBeamThreads / 64) * 64 + 63 - lane]);
+    return __shfl(v, n - 1);
+}
+
+// ---- stage 1: the n best of a segment of a row, and its part of the log-normaliser ----
+// A segment passes through registers once, kChunk categories at a time.  The n-th largest of the first chunk's 256 thread maxima is a
+// bound that at least n categories reach; what reaches it (some 1.1 n of a chunk) goes to a list in LDS, and later chunks add
+// what lies above it, for a category further back loses a tie.  Should the list overflow (rows in ascending order, ties), the bound is
+// raised by the chunk's own maxima, then by the list cut to its n best, and as a last resort the chunk goes through the list 256 at a time.
+constexpr int kElems = 16, kChunk = kBeamThreads * kElems, kList = 1024;
+struct RowPart { float m; float pad; double sum; };    // maximum and sum of exp(z - m) of a segment
+
+template <typename T> struct Vec { static constexpr int N = 16 / sizeof(T); };
+
+// The categories of a chunk: virtual index i (category + off, where off is the row's distance from a 16-byte boundary) of element e.
+template <typename T>
+__device__ inline int64_t elem_index(int64_t base, int e)
+{
+    constexpr int N = Vec<T>::N;
+    return base + (e / N) * (kBeamThreads * N) + threadIdx.x * N + e % N;
+}
+// -inf outside [lo, hi)
+template <typename T>
+__device__ inline void load_chunk(const T *row, int64_t base, int64_t lo, int64_t hi, float (&v)[kElems])
+{
+    constexpr int N = Vec<T>::N;
+#pragma unroll
+    for (int j = 0; j < kElems / N; ++j) {
+        const int64_t i = elem_index<T>(base, j * N);
+        if (i >= lo && i + N <= hi) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(row + i);
+            const T *t = reinterpret_cast<const T *>(&q);
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[j * N + k] = to_f32(t[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[j * N + k] = i + k >= lo && i + k < hi ? to_f32(row[i + k]) : PC_NEG_INF_F;
         }
-        if (threadIdx.x == 0) lse[r] = norm;
     }
 }
 
-// The n best of a group's beams * n_out row survivors, one workgroup a group, one pass per survivor.
-__global__ __launch_bounds__(kBeamThreads) void k_beam_join(const BeamDev a, const uint64_t *__restrict__ best, const double *__restrict__ lse,
-                                                            float *__restrict__ out_scores, int32_t *__restrict__ parents, int32_t *__restrict__ tokens)
+struct BeamLds {
+    uint64_t list[kList], kept[64];
+    float nth[kBeamThreads];
+    int count;
+};
+
+// Cut the list to its n best, in order; returns the n-th (0: fewer).  All threads; the list is complete and synchronised.
+__device__ inline uint64_t cut_list(BeamLds &s, int n)
 {
-    __shared__ double top_s[kBeamThreads / 64];
-    __shared__ int32_t top_i[kBeamThreads / 64];
-    const int n_cand = a.beams * a.n_out;
-    // candidate i of group g: its score (NaN: no such candidate) and its category
-    auto look = [&](int64_t g, int i, double &score, int32_t &token) {
-        const int64_t r = g * a.beams + i / a.n_out;
-        const int at = i % a.n_out;
-        const double run = (double)running_score(a, r), norm = lse[r];
-        const bool done = a.done && a.done[r], dead = run == kNegInf64 || !(fabs(norm) < 1e300);
-        if (at >= a.n_cats) { score = __builtin_nan(""); token = 0; return; }
-        if (dead) { score = kNegInf64; token = at; return; }
-        if (done) {
-            token = at == 0 ? a.done_token : at <= a.done_token ? at - 1 : at;
-            score = at == 0 ? run : kNegInf64;
-            return;
+    int count = s.count;
+    if (count > 128) {                                 // a bound from thread maxima leaves few for the ranking
+        float mine = PC_NEG_INF_F;
+        for (int i = threadIdx.x; i < count; i += kBeamThreads) mine = fmaxf(mine, key_value((uint32_t)(s.list[i] >> 32)));
+        const uint32_t bound = order_key(block_nth(mine, n, s.nth));
+        uint64_t held[kList / kBeamThreads];
+#pragma unroll
+        for (int i = 0; i < kList / kBeamThreads; ++i) held[i] = threadIdx.x + i * kBeamThreads < count ? s.list[threadIdx.x + i * kBeamThreads] : 0;
+        __syncthreads();
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kList / kBeamThreads; ++i)
+            if (held[i] && (uint32_t)(held[i] >> 32) >= bound) s.list[atomicAdd(&s.count, 1)] = held[i];
+        __syncthreads();
+        count = s.count;
+    }
+    if (threadIdx.x < 64) s.kept[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += kBeamThreads) {
+        const uint64_t k = s.list[i];
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += s.list[j] > k;
+        if (rank < n) s.kept[rank] = k;
+    }
+    __syncthreads();
+    if (threadIdx.x < n) s.list[threadIdx.x] = s.kept[threadIdx.x];
+    if (threadIdx.x == 0) s.count = min(count, n);
+    __syncthreads();
+    return s.kept[n - 1];
+}
+
+// the next float up; above +inf: NaN, which nothing reaches
+__device__ inline float next_above(float t) { return key_value(order_key(t) + 1); }
+
+template <typename T>
+__global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int32_t n_seg, int32_t seg_len, uint64_t *__restrict__ best,
+                                                            RowPart *__restrict__ parts)
+{
+    __shared__ BeamLds s;
+    __shared__ float wave_m[kBeamThreads / 64];
+    __shared__ double wave_sum[kBeamThreads / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n_out;
+    const int64_t tasks = (int64_t)a.groups * a.beams * n_seg;
+    for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+        const int64_t r = task / n_seg;
+        if ((a.done && a.done[r]) || running_score(a, r) == PC_NEG_INF_F) continue;       // the join knows these beams' candidates
+        const T *z = (const T *)a.scores + r * a.ld;
+        const int64_t off = ((uintptr_t)z & 15) / sizeof(T);
+        const T *row = z - off;                        // category c is element c + off; none before off is read
+        const int64_t first = (task % n_seg) * (int64_t)seg_len, hi = min(off + a.n_cats, first + seg_len), lo = max(off, first);
+        float m = PC_NEG_INF_F, sum = 0.0f, t = PC_NEG_INF_F;
+        __syncthreads();
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+        float v[kElems], ahead[kElems];
+        load_chunk(row, first, lo, hi, ahead);
+        for (int64_t base = first; base < hi; base += kChunk) {
+#pragma unroll
+            for (int e = 0; e < kElems; ++e) v[e] = ahead[e];
+            if (base + kChunk < hi) load_chunk(row, base + kChunk, lo, hi, ahead);
+            float top = v[0];
+#pragma unroll
+            for (int e = 1; e < kElems; ++e) top = fmaxf(top, v[e]);
+            top = fmaxf(top, PC_NEG_INF_F);            // NaN alone
+            if (a.normalise) {
+                if (top > m) { sum *= exp2f((m - top) * PC_LOG2E_F); m = top; }
+                const float at = m == PC_NEG_INF_F ? 0.0f : m;
+                float part = 0.0f;
+#pragma unroll
+                for (int e = 0; e < kElems; ++e) part += __builtin_amdgcn_exp2f((v[e] - at) * PC_LOG2E_F);
+                sum += part;
+            }
+            bool fresh = false, slow = false;          // fresh: t is reached by n categories of this chunk or before
+            if (t == PC_NEG_INF_F) {
+                t = block_nth(top, n, s.nth);
+                fresh = t > PC_NEG_INF_F;
+                slow = !fresh;
+            }
+            // count what reaches t; room for all of it, or a higher t
+            int mine = 0, at = 0;
+            for (int attempt = 0; !slow; ++attempt) {
+                mine = 0;
+#pragma unroll
+                for (int e = 0; e < kElems; ++e) mine += __popcll(__ballot(v[e] >= t));
+                __syncthreads();
+                if (lane == 0 && mine) at = atomicAdd(&s.count, mine);
+                __syncthreads();
+                const int total = s.count;
+                if (total <= kList) break;
+                __syncthreads();
+                if (lane == 0 && mine) atomicSub(&s.count, mine);
+                __syncthreads();
+                if (attempt == 0) {
+                    const float bound = block_nth(top, n, s.nth);
+                    if (!(bound < t)) { t = bound; fresh = true; }
+                } else if (attempt == 1) {
+                    const uint64_t nth = cut_list(s, n);
+                    const float bound = nth ? next_above(key_value((uint32_t)(nth >> 32))) : t;
+                    if (bound > t || bound != bound) { t = bound; fresh = false; }
+                } else {
+                    slow = true;
+                }
+            }
+            if (!slow) {
+                at = __shfl(at, 0);
+                if (mine)
+#pragma unroll
+                    for (int e = 0; e < kElems; ++e) {
+                        const uint64_t on = __ballot(v[e] >= t);
+                        if (on == 0) continue;
+                        if (v[e] >= t) s.list[at + __popcll(on & ((1ull << lane) - 1))] = candidate(v[e], (int)(elem_index<T>(base, e) - off));
+                        at += __popcll(on);
+                    }
+                if (fresh) t = next_above(t);
+            } else {
+                uint64_t above = 0;                    // only keys above this one count
+                for (int e = 0; e < kElems; ++e) {
+                    __syncthreads();
+                    const bool full = s.count > kList - kBeamThreads;
+                    __syncthreads();                   // all have read it before any adds
+                    if (full) above = cut_list(s, n);
+                    float x = v[0];
+#pragma unroll
+                    for (int f = 1; f < kElems; ++f) x = f == e ? v[f] : x;
+                    const int64_t i = elem_index<T>(base, e);
+                    const uint64_t k = i >= lo && i < hi ? candidate(x, (int)(i - off)) : 0;
+                    if (k > above) s.list[atomicAdd(&s.count, 1)] = k;
+                }
+                __syncthreads();
+                const uint64_t nth = cut_list(s, n);
+                t = nth ? next_above(key_value((uint32_t)(nth >> 32))) : PC_NEG_INF_F;
+            }
         }
-        const uint64_t k = best[r * a.n_out + at];
-        score = run + ((double)key_value((uint32_t)(k >> 32)) - norm);
-        token = (int32_t)~(uint32_t)k;
-    };
-    for (int64_t g = blockIdx.x; g < a.groups; g += gridDim.x) {
-        double last_s = 0.0;
-        int last_i = -1;
-        for (int n = 0; n < a.n_out; ++n) {
-            double mine = 0.0;
-            int at = -1;
-            for (int i = threadIdx.x; i < n_cand; i += kBeamThreads) {
-                double s;
-                int32_t token;
-                look(g, i, s, token);
-                if (s != s) continue;
-                const bool left = last_i < 0 || s < last_s || (s == last_s && i > last_i);
-                if (left && (at < 0 || s > mine)) { mine = s; at = i; }
-            }
-            for (int d = 32; d > 0; d >>= 1) {
-                const double s = __shfl_xor(mine, d);
-                const int i = __shfl_xor(at, d);
-                if (i >= 0 && (at < 0 || s > mine || (s == mine && i < at))) { mine = s; at = i; }
-            }
+        __syncthreads();
+        cut_list(s, n);
+        if (threadIdx.x < n) best[task * n + threadIdx.x] = s.kept[threadIdx.x];
+        if (a.normalise) {
+            float all = m;
+            for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d));
+            if (lane == 0) wave_m[wave] = all;
             __syncthreads();
-            if (threadIdx.x % 64 == 0) { top_s[threadIdx.x / 64] = mine; top_i[threadIdx.x / 64] = at; }
+            for (int w = 0; w < kBeamThreads / 64; ++w) all = fmaxf(all, wave_m[w]);
+            double total = (double)sum * (m == PC_NEG_INF_F ? 1.0 : (double)exp2f((m - all) * PC_LOG2E_F));
+            for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+            if (lane == 0) wave_sum[wave] = total;
             __syncthreads();
-            at = -1;
-            for (int w = 0; w < kBeamThreads / 64; ++w)
-                if (top_i[w] >= 0 && (at < 0 || top_s[w] > mine || (top_s[w] == mine && top_i[w] < at))) { mine = top_s[w]; at = top_i[w]; }
             if (threadIdx.x == 0) {
-                double s;
-                int32_t token;
-                look(g, at, s, token);
-                out_scores[g * a.n_out + n] = (float)s;
-                parents[g * a.n_out + n] = at / a.n_out;
-                tokens[g * a.n_out + n] = token;
+                total = 0.0;
+                for (int w = 0; w < kBeamThreads / 64; ++w) total += wave_sum[w];
+                parts[task] = RowPart{all, 0.0f, total};
             }
-            last_s = mine;
-            last_i = at;
+        }
+    }
+}
+
+// ---- stage 2: a group's survivors from its rows' lists ----
+// A wave a beam (up to 16 waves, each taking several beams in turn): the segments' parts of the log-normaliser in 64 bits, the segments'
+// lists merged by key, then by score with the wave's beams before; last the waves' lists, half of them at a time.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(const BeamDev a, int32_t n_seg, const uint64_t *__restrict__ best,
+                                                               const RowPart *__restrict__ parts, float *__restrict__ out_scores,
+                                                               int32_t *__restrict__ parents, int32_t *__restrict__ tokens)
+{
+    __shared__ Cand lists[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, n = a.n_out;
+    const Cand none{kNegInf64, kNoPlace, 0};
+    for (int64_t g = blockIdx.x; g < a.groups; g += gridDim.x) {
+        Cand mine = none;
+        for (int b = wave; b < a.beams; b += waves) {
+            const int64_t r = g * a.beams + b;
+            const double run = (double)running_score(a, r);
+            const bool done = a.done && a.done[r];
+            bool dead = run == kNegInf64;
+            Cand c = none;
+            if (!dead && !done) {
+                double norm = 0.0;
+                if (a.normalise) {
+                    float m = PC_NEG_INF_F;
+                    double sum = 0.0;
+                    for (int i = lane; i < n_seg; i += 64) m = fmaxf(m, parts[r * n_seg + i].m);
+                    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+                    for (int i = lane; i < n_seg; i += 64) {
+                        const RowPart p = parts[r * n_seg + i];
+                        sum += p.m == PC_NEG_INF_F ? p.sum : p.sum * exp((double)p.m - (double)m);
+                    }
+                    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+                    norm = (double)m + log(sum);
+                }
+                dead = !(fabs(norm) < 1e300);          // no finite number: m is a float
+                uint64_t key = 0;
+                for (int s0 = 0; s0 < n_seg; s0 += 8) {
+                    uint64_t next[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        next[i] = s0 + i < n_seg && (s0 + i == 0 ? lane : 63 - lane) < n ? best[(r * n_seg + s0 + i) * n + (s0 + i == 0 ? lane : 63 - lane)] : 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (s0 + i == 0) key = next[i];
+                        else if (s0 + i < n_seg) key = merge_lanes(key, next[i]);
+                }
+                if (key && lane < n) c = Cand{run + ((double)key_value((uint32_t)(key >> 32)) - norm), (uint32_t)(b << 8 | lane), (int32_t)~(uint32_t)key};
+            }
+            if (dead || done) {                        // candidates of -inf in order, after the one of a finished beam
+                const bool ended = done && !dead;
+                const int token = !ended ? lane : lane == 0 ? a.done_token : lane <= a.done_token ? lane - 1 : lane;
+                c = lane < min(n, a.n_cats) ? Cand{ended && lane == 0 ? run : kNegInf64, (uint32_t)(b << 8 | lane), token} : none;
+            }
+            if (b == wave) mine = c;
+            else mine = merge_lanes(mine, Cand{__shfl(c.score, 63 - lane), (uint32_t)__shfl((int)c.place, 63 - lane), __shfl(c.token, 63 - lane)});
+        }
+        for (int half = waves; half > 1;) {
+            const int keep = (half + 1) / 2;
+            __syncthreads();
+            if (wave >= keep && wave < half) lists[wave][lane] = mine;
+            __syncthreads();
+            if (wave + keep < half) mine = merge_lanes(mine, lists[wave + keep][63 - lane]);
+            half = keep;
+        }
+        if (wave == 0 && lane < n) {
+            out_scores[g * n + lane] = (float)mine.score;
+            parents[g * n + lane] = (int32_t)(mine.place >> 8);
+            tokens[g * n + lane] = mine.token;
         }
     }
 }
@@ -183,7 +405,18 @@ static pc_status check_beam(const pc_beam *a)
     if (!aligned_to(a->scores, type_bytes(a->scores_type)) || !aligned_to(a->running, 4)) return fail(PC_ERR_ARG, "arrays must be aligned to their elements");
     return PC_OK;
 }
-static size_t best_bytes(const pc_beam *a) { return ((size_t)a->groups * a->beams * a->n_out * 8 + 15) / 16 * 16; }
+// Segments of a row: enough workgroups for four a CU, but none shorter than a chunk.  (The offset of a row from its 16-byte boundary
+// makes it up to seven elements longer.)
+struct Segments { int32_t n, len; };
+static Segments segments_of(const pc_beam *a)
+{
+    const int64_t rows = (int64_t)a->groups * a->beams, len = (int64_t)a->n_cats + 7, chunks = (len + kChunk - 1) / kChunk;
+    const int64_t most = (1 << 30) / kChunk;           // chunks of a segment whose length is an int32
+    const int64_t wanted = std::min(chunks, std::max(1024 / std::max<int64_t>(rows, 1), (chunks + most - 1) / most));
+    const int64_t each = (chunks + wanted - 1) / wanted;
+    return Segments{(int32_t)((chunks + each - 1) / each), (int32_t)(each * kChunk)};
+}
+static size_t best_bytes(const pc_beam *a) { return ((size_t)a->groups * a->beams * segments_of(a).n * a->n_out * 8 + 15) / 16 * 16; }
 
 }  // namespace pc
 
@@ -196,7 +429,7 @@ pc_status pc_beam_workspace_bytes(const pc_beam *a, size_t *bytes)
     const pc_status st = check_beam(a);
     if (st != PC_OK) return st;
     if (!bytes) return fail(PC_ERR_ARG, "NULL argument");
-    *bytes = best_bytes(a) + (size_t)a->groups * a->beams * 8;
+    *bytes = best_bytes(a) + (size_t)a->groups * a->beams * segments_of(a).n * sizeof(RowPart);
     return PC_OK;
 }
 
@@ -211,12 +444,14 @@ pc_status pc_beam_select(const pc_beam *a, void *workspace, size_t workspace_byt
     pc_beam_workspace_bytes(a, &need);
     if (workspace_bytes < need) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_beam_workspace_bytes");
     const BeamDev dev{a->groups, a->beams, a->n_cats, a->n_out, a->scores, a->scores_ld, a->normalise != 0, a->running, a->done, a->done_token};
+    const Segments seg = segments_of(a);
     uint64_t *best = (uint64_t *)workspace;
-    double *lse = (double *)((char *)workspace + best_bytes(a));
+    RowPart *parts = (RowPart *)((char *)workspace + best_bytes(a));
     const hipStream_t s = (hipStream_t)stream;
-    const unsigned rows = (unsigned)std::min<int64_t>((int64_t)a->groups * a->beams, 1 << 20);
-    with_type(a->scores_type, [&](auto t) { hipLaunchKernelGGL((k_beam_rows<decltype(t)>), dim3(rows), dim3(kBeamThreads), 0, s, dev, best, lse); });
-    hipLaunchKernelGGL(k_beam_join, dim3((unsigned)std::min(a->groups, 1 << 20)), dim3(kBeamThreads), 0, s, dev, best, lse, out_scores, parents, tokens);
+    const unsigned tasks = (unsigned)std::min<int64_t>((int64_t)a->groups * a->beams * seg.n, 1 << 20);
+    with_type(a->scores_type, [&](auto t) { hipLaunchKernelGGL((k_beam_rows<decltype(t)>), dim3(tasks), dim3(kBeamThreads), 0, s, dev, seg.n, seg.len, best, parts); });
+    hipLaunchKernelGGL(k_beam_join, dim3((unsigned)std::min(a->groups, 1 << 20)), dim3((unsigned)(64 * std::min(a->beams, kJoinWaves))), 0, s, dev, seg.n, best,
+                       parts, out_scores, parents, tokens);
     return launched();
 }
 
