@@ -96,107 +96,191 @@ __device__ inline floatx16 mfma(const uint4 &a, const uint4 &b, const floatx16 &
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Predictive distribution.  A wave owns 32 categories x 32 NT samples; a workgroup WAVES * 32 categories of the same samples.  States come
-// in chunks of KC: each lane fetches its category's table row (8 contiguous states a step of 16, split in registers, read once from
-// memory), the workgroup stages the weights [states][samples] into LDS as planes in operand order, both one chunk ahead, one barrier a chunk.
-// Products hi*hi + hi*lo + lo*hi.  The samples are the instruction's rows, so that a store covers 32 neighbouring categories.
-// Where a group of four states begins in the tables and in the weights is looked up in LDS, a window of states at a time: blocks need not be
-// as long as a chunk.
+// Predictive distribution.  A wave owns 32 categories x 32 NT samples and, of each chunk of KC * SPLIT states, its KC: with SPLIT > 1 (few
+// samples: waves with little to add up, bound by loads in flight) SPLIT waves of a workgroup share categories and add their sums at the end.
+// Each lane fetches its category's table row (8 contiguous states a step of 16, split in registers, read once from memory); the workgroup
+// stages the weights [states][samples] into LDS as planes in operand order.  While a chunk is multiplied the next one is split and staged
+// and the one after it is on its way; one barrier a chunk.  Products of planes down to the last order kept (two planes: hi*hi + hi*lo + lo*hi; three: six).  The samples are the instruction's rows, so that a
+// store covers 32 neighbouring categories.
+// PLANES = 3: all six products down to 2^-24.
+// Where a group of four states begins in the tables and in the weights is looked up in LDS, a window of states at a time, so that
+// blocks need not be as long as a chunk; WHOLE: they are multiples of KC, one look-up serves a wave's part.
 constexpr int kWindow = 2048;
-template <int NT, int WAVES, int KC>
-__global__ __launch_bounds__(64 * WAVES, NT == 8 ? 2 : 3) void k_predict(const pc_mixture m, const float *__restrict__ tables, int32_t B,
+template <int NT, int WAVES, int SPLIT, int KC, int PLANES, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 3 : 4) void k_predict(const pc_mixture m, const float *__restrict__ tables, int32_t B,
                                                                         float *__restrict__ logp, int64_t ld)
 {
-    constexpr int TH = 64 * WAVES, NB = 32 * NT, STEPS = KC / 16, TASKS = NB * KC / 8, FT = (TASKS + TH - 1) / TH;
-    __shared__ uint4 planes[2][2][KC / 8][NB];        // [buffer][hi, lo][8 states][sample]
+    constexpr int TH = 64 * WAVES, NB = 32 * NT, STEPS = KC / 16, KW = KC * SPLIT, TASKS = NB * KW / 8, FT = (TASKS + TH - 1) / TH;
+    __shared__ uint4 planes[2][PLANES][KW / 8][NB];   // [buffer][plane][8 states][sample]
     __shared__ int64_t t_at[kWindow / 4], w_at[kWindow / 4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
-    const int H = m.n_blocks * m.K, c0 = (blockIdx.x * WAVES + wave) * 32, b0 = blockIdx.y * NB;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5, part = wave % SPLIT;
+    const int H = m.n_blocks * m.K, c0 = (blockIdx.x * (WAVES / SPLIT) + wave / SPLIT) * 32, b0 = blockIdx.y * NB;
     const int64_t mine = (int64_t)min(c0 + col, m.n_cats - 1) * m.K;     // a category behind the last reads that one's row again
+    const int here = min(NB, B - b0);                  // samples of this workgroup
     floatx16 acc[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[t][e] = 0.0f;
+    // A thread's eight weights of a chunk: sample, group of eight states.  Of 32 columns only those with a sample are staged, -1: none.
+    int task_b[FT], task_g[FT];
+    bool wave_stages[FT];                              // the same for all lanes: some lane has weights to stage
+#pragma unroll
+    for (int f = 0; f < FT; ++f) {
+        const int task = threadIdx.x + f * TH, width = NT == 1 ? here : NB;
+        task_b[f] = task % width;
+        task_g[f] = NT > 1 || task / width < KW / 8 ? task / width : -1;
+        wave_stages[f] = NT > 1 || __builtin_amdgcn_readfirstlane(__ballot(task_g[f] >= 0) != 0);
+    }
+    static_assert(NT == 1 || TASKS % TH == 0, "every thread has FT tasks");
 
     auto fill_window = [&](int n0) {
         for (int i = threadIdx.x; i < kWindow / 4; i += TH) {
             const int n = n0 + 4 * i;
-            int64_t t = -1, w = -1;
-            if (n < H) {
-                const MixBlock blk = mix_block(m, n / m.K);
-                if (blk.row >= 0) { t = (int64_t)blk.table * m.n_cats * m.K + n % m.K; w = (blk.row + n % m.K) * m.stride; }
-            }
-            t_at[i] = t;
-            w_at[i] = w;
+            const MixBlock blk = n < H ? mix_block(m, n / m.K) : MixBlock{-1, -1};
+            t_at[i] = blk.row >= 0 ? (int64_t)blk.table * m.n_cats * m.K + n % m.K : -1;
+            w_at[i] = blk.row >= 0 ? (blk.row + n % m.K) * m.stride : -1;
         }
     };
+    // What lies outside (blocks left out, states behind the last, samples behind B) is read from a place that exists and masked when it is
+    // split.  A chunk behind the last state is fetched and staged like any other, and not used.
     float4 t_raw[STEPS][2];
     float w_raw[FT][8];
-    auto fetch = [&](int n0) {                         // n0: first state of the chunk
+    uint32_t t_mask[WHOLE ? 1 : STEPS][2], w_mask[FT][2];
+    auto fetch_weights = [&](int n0, int f) {          // of the chunk that begins with state n0
         const int g0 = n0 % kWindow / 4;
+        if (!wave_stages[f]) return;
+        const int b = min(task_b[f], here - 1);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+        for (int q = 0; q < 2; ++q) {
+            const int64_t at = task_g[f] >= 0 && task_b[f] < here ? w_at[g0 + 2 * task_g[f] + q] : -1;
+            const float *src = m.weights + (at >= 0 ? at : 0) + b0 + b;
+            w_mask[f][q] = at >= 0 ? ~0u : 0u;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int64_t at = t_at[g0 + 4 * s + 2 * half + q];
-                const float4 v = *reinterpret_cast<const float4 *>(tables + (at >= 0 ? at + mine : 0));
-                t_raw[s][q] = at >= 0 ? v : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-        for (int f = 0; f < FT; ++f) {
-            const int task = threadIdx.x + f * TH, b = task % NB, g = task / NB;
-            const bool on = (TASKS % TH == 0 || task < TASKS) && b0 + b < B;
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int64_t at = on ? w_at[g0 + 2 * g + q] : -1;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w_raw[f][4 * q + i] = at >= 0 ? m.weights[at + i * m.stride + b0 + b] : 0.0f;
-            }
+            for (int i = 0; i < 4; ++i) w_raw[f][4 * q + i] = src[i * m.stride];
         }
     };
+    auto fetch_tables = [&](int n0) {
+        const int g0 = n0 % kWindow / 4;
+        if (WHOLE) {
+            const int64_t v = t_at[g0 + part * (KC / 4)];
+            const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+            const float *src = tables + (at >= 0 ? at : 0) + (mine + 8 * half);
+            t_mask[0][0] = at >= 0 ? ~0u : 0u;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) t_raw[s][q] = *reinterpret_cast<const float4 *>(src + 16 * s + 4 * q);
+        } else {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int64_t at = t_at[g0 + part * (KC / 4) + 4 * s + 2 * half + q];
+                    t_mask[s][q] = at >= 0 ? ~0u : 0u;
+                    t_raw[s][q] = *reinterpret_cast<const float4 *>(tables + (at >= 0 ? at : 0) + mine);
+                }
+        }
+    };
+    auto masked = [](float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask) * kUp; };
+    auto stage_weights = [&](int buf, int f) {
+        if (!wave_stages[f]) return;
+        float x[8];
+        uint4 pl[PLANES];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = masked(w_raw[f][i], w_mask[f][i / 4]);
+        split8(x, pl);
+        if (NT > 1 || task_g[f] >= 0)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) planes[buf][p][task_g[f]][task_b[f]] = pl[p];
+    };
+    uint4 tp[STEPS][PLANES];
+    auto split_tables = [&](int s) {
+        const float4 u = t_raw[s][0], v = t_raw[s][1];
+        const uint32_t m0 = t_mask[WHOLE ? 0 : s][0], m1 = t_mask[WHOLE ? 0 : s][WHOLE ? 0 : 1];
+        const float x[8] = {masked(u.x, m0), masked(u.y, m0), masked(u.z, m0), masked(u.w, m0), masked(v.x, m1), masked(v.y, m1), masked(v.z, m1), masked(v.w, m1)};
+        split8(x, tp[s]);
+    };
 
+    if (NT == 1 && here < NB)                          // columns without a sample stay zero
+        for (int i = threadIdx.x; i < (int)(sizeof(planes) / 16); i += TH) (&planes[0][0][0][0])[i] = make_uint4(0, 0, 0, 0);
     fill_window(0);
     __syncthreads();
-    fetch(0);
-    for (int n0 = 0, buf = 0; n0 < H; n0 += KC, buf ^= 1) {
 #pragma unroll
-        for (int f = 0; f < FT; ++f) {
-            const int task = threadIdx.x + f * TH;
-            if (TASKS % TH != 0 && task >= TASKS) break;
-            float x[8];
-            uint4 pl[2];
+    for (int f = 0; f < FT; ++f) fetch_weights(0, f);
+    fetch_tables(0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = w_raw[f][i] * kUp;
-            split8(x, pl);
-            planes[buf][0][task / NB][task % NB] = pl[0];
-            planes[buf][1][task / NB][task % NB] = pl[1];
-        }
-        uint4 th[STEPS], tl[STEPS];
+    for (int f = 0; f < FT; ++f) { stage_weights(0, f); fetch_weights(KW, f); }
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const float4 u = t_raw[s][0], v = t_raw[s][1];
-            const float x[8] = {u.x * kUp, u.y * kUp, u.z * kUp, u.w * kUp, v.x * kUp, v.y * kUp, v.z * kUp, v.w * kUp};
-            uint4 pl[2];
-            split8(x, pl);
-            th[s] = pl[0];
-            tl[s] = pl[1];
-        }
-        __syncthreads();                               // the chunk's planes are there, and everyone has read the window for it
-        const int next = n0 + KC;
-        if (next < H) {
-            if (next % kWindow == 0) { fill_window(next); __syncthreads(); }
-            fetch(next);
-        }
+    for (int s = 0; s < STEPS; ++s) split_tables(s);
+    fetch_tables(KW);
+    __syncthreads();
+    // An iteration is STEPS * NT / G slices of 3 G products, among which the work for the next chunk is dealt out: the two waves of a SIMD
+    // then find something for the vector ALU while the other one's products run.
+    constexpr int G = NT > 1 ? 2 : 1, SLICES = STEPS * NT / G;
+    for (int n0 = 0, buf = 0; n0 < H; n0 += KW, buf ^= 1) {
+        const int next = n0 + 2 * KW;
+        if (next % kWindow == 0) { fill_window(next); __syncthreads(); }                   // the barrier before: all have read the last one
+        uint4 cp[STEPS][PLANES], wp[2][G][PLANES];
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const uint4 wh = planes[buf][0][2 * s + half][32 * t + col], wl = planes[buf][1][2 * s + half][32 * t + col];
-                acc[t] = mfma(wl, th[s], acc[t]);
-                acc[t] = mfma(wh, tl[s], acc[t]);
-                acc[t] = mfma(wh, th[s], acc[t]);
+            for (int p = 0; p < PLANES; ++p) cp[s][p] = tp[s][p];
+        auto operands = [&](int slice) {
+            const int s = slice / (NT / G), t = slice % (NT / G) * G;
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) wp[slice & 1][g][p] = planes[buf][p][part * (KC / 8) + 2 * s + half][32 * (t + g) + col];
+        };
+        auto tables_on = [&]() {
+#pragma unroll
+            for (int q = 0; q < STEPS; ++q) split_tables(q);
+            fetch_tables(next);
+        };
+        if (NT == 1) {                                 // bound by the loads: they leave first
+#pragma unroll
+            for (int f = 0; f < FT; ++f) { stage_weights(buf ^ 1, f); fetch_weights(next, f); }
+            tables_on();
+        }
+        operands(0);
+#pragma unroll
+        for (int slice = 0; slice < SLICES; ++slice) {
+            const int s = slice / (NT / G), t = slice % (NT / G) * G, o = slice & 1;
+            if (slice + 1 < SLICES) operands(slice + 1);
+#pragma unroll
+            for (int sum = PLANES - 1; sum >= 0; --sum)  // the small products first
+#pragma unroll
+                for (int p = sum; p >= 0; --p)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) acc[t + g] = mfma(wp[o][g][p], cp[s][sum - p], acc[t + g]);
+            if (NT > 1) {
+#pragma unroll
+                for (int f = 0; f < FT; ++f)
+                    if (f * SLICES / FT == slice) { stage_weights(buf ^ 1, f); fetch_weights(next, f); }
+                if (slice == SLICES - 1) tables_on();
+                __builtin_amdgcn_sched_barrier(0);
             }
+        }
+        __syncthreads();
+    }
+    static_assert(kWindow % KW == 0 && kWindow >= 4 * KW, "a chunk lies in one window, the first two in the first");
+    if (SPLIT > 1) {                                   // sums of the other parts, half of them at a time, through the planes' memory
+        float *sums = reinterpret_cast<float *>(&planes[0][0][0][0]);
+        static_assert(SPLIT == 1 || (NT == 1 && sizeof(planes) >= WAVES / 2 * 16 * 64 * 4), "half the waves' sums fit");
+#pragma unroll
+        for (int h = SPLIT / 2; h > 0; h /= 2) {
+            float *slot = sums + (wave / SPLIT * h + part % h) * 16 * 64 + lane;
+            if (part >= h && part < 2 * h)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) slot[e * 64] = acc[0][e];
+            __syncthreads();
+            if (part < h)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[0][e] += slot[e * 64];
+            __syncthreads();
+        }
+        if (part != 0) return;
     }
     if (c0 + col >= m.n_cats) return;
 #pragma unroll
@@ -207,6 +291,84 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 ? 2 : 3) void k_predict(const p
             const float p = acc[t][e] * (kDown * kDown);
             if (b < B) logp[(int64_t)b * ld + c0 + col] = p < __FLT_MIN__ ? PC_NEG_INF_F : logf(p);
         }
+}
+
+// A few samples: bound by reading the tables once.  The lanes of a wave cover whole table rows (K / 4 lanes each with four states) of the
+// same block, so that loads are contiguous, kFewRows of two blocks in flight; a lane keeps its states' weights of the block in registers
+// and a sum per row and sample, and only at the end of all blocks the lanes of a row add theirs.  Products in fp32.
+constexpr int kFewFloats = 4096, kFewRows = 8;         // weights in LDS at a time; loads of a lane in flight, of two blocks each
+template <int NS>
+__global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const float *__restrict__ tables, int32_t B, float *__restrict__ logp, int64_t ld)
+{
+    __shared__ float4 w[kFewFloats / 4];              // [block of the window][sample][piece]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int P = m.K / 4, R = 64 / P, piece = lane % P, r = lane / P;      // pieces of a row, rows of an instruction
+    const bool idle = r >= R;
+    const int per_window = min(m.n_blocks, kFewFloats / (NS * m.K));        // at least 16: K <= 128, NS <= 2
+    const int64_t c0 = ((int64_t)blockIdx.x * 4 + wave) * R * kFewRows + (idle ? 0 : r);
+    float acc[kFewRows][NS];
+    bool on[2];
+#pragma unroll
+    for (int u = 0; u < kFewRows; ++u)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) acc[u][s] = 0.0f;
+    int64_t row[kFewRows];                                 // a category behind the last reads that one's row again
+#pragma unroll
+    for (int u = 0; u < kFewRows; ++u) row[u] = min(c0 + u * R, (int64_t)m.n_cats - 1) * m.K + 4 * piece;
+    for (int j0 = 0; j0 < m.n_blocks; j0 += per_window) {
+        const int here = min(per_window, m.n_blocks - j0);
+        __syncthreads();
+        for (int i = threadIdx.x; i < here * P * NS; i += 256) {
+            const int b = i % NS, q = i / NS % P, j = i / (NS * P);
+            const MixBlock blk = mix_block(m, j0 + j);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (blk.row >= 0 && b < B) {
+                const float *src = m.weights + (blk.row + 4 * q) * m.stride + b;
+                v = make_float4(src[0], src[m.stride], src[2 * m.stride], src[3 * m.stride]);
+            }
+            w[(j * NS + b) * P + q] = v;
+        }
+        __syncthreads();
+        float4 t[2][kFewRows];                             // a block's rows, while those of the one before are added up
+        auto fetch = [&](int j, int set) {             // a block left out reads the first table's rows and is not added
+            const MixBlock blk = mix_block(m, j0 + j);
+            on[set] = blk.row >= 0;
+            const float *src = tables + (int64_t)max(blk.table, 0) * m.n_cats * m.K;
+#pragma unroll
+            for (int u = 0; u < kFewRows; ++u) t[set][u] = *reinterpret_cast<const float4 *>(src + row[u]);
+        };
+        auto add = [&](int j, int set) {
+            if (!on[set]) return;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const float4 v = w[(j * NS + s) * P + piece];
+#pragma unroll
+                for (int u = 0; u < kFewRows; ++u) acc[u][s] += t[set][u].x * v.x + t[set][u].y * v.y + t[set][u].z * v.z + t[set][u].w * v.w;
+            }
+        };
+        fetch(0, 0);
+        for (int j = 0; j < here; j += 2) {
+            fetch(min(j + 1, here - 1), 1);
+            add(j, 0);
+            if (j + 1 < here) {
+                fetch(min(j + 2, here - 1), 0);
+                add(j + 1, 1);
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kFewRows; ++u) {
+        const int64_t c = c0 + u * R;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            float v = acc[u][s];
+            for (int d = 1; d < P; d <<= 1) {          // lane `piece` adds d lanes more each time, none of another row
+                const float o = __shfl_down(v, d);
+                if (piece + d < P && piece % (2 * d) == 0) v += o;
+            }
+            if (piece == 0 && !idle && s < B && c < m.n_cats) logp[s * ld + c] = v < __FLT_MIN__ ? PC_NEG_INF_F : logf(v);
+        }
+    }
 }
 
 // g / p of one sample and category; p = 0 adds nothing
@@ -256,21 +418,38 @@ __global__ __launch_bounds__(256) void k_predict_flow_any(const pc_mixture m, co
             }
 }
 
+// One or two samples of many categories: no matrix cores (4096 states x 50257 at one sample: 171 us against 211 with them, at four 212 against 200),
+// where that makes waves enough for two to a CU.
 // Samples a wave: as many of 256 as there are, so that the tables are read once; fewer where that leaves a SIMD without a wave (the
 // tables of few categories stay in the caches).
+// Two planes an operand where log-probabilities are large (many categories), three where they are not: an error of 2^-18 of a probability
+// is 10^-6 of a logarithm of -4, but as much as the logarithm's own rounding allows at -10.
 static void launch_predict(const pc_mixture &m, const float *tables, int32_t B, float *logp, int64_t ld, hipStream_t s)
 {
+    const int64_t few_rows = 64 / (m.K / 4) * kFewRows;                  // categories of a wave
+    if (B <= 2 && m.n_cats >= 512 * few_rows) {
+        const dim3 grid((unsigned)((m.n_cats + 4 * few_rows - 1) / (4 * few_rows)));
+        if (B == 1) hipLaunchKernelGGL((k_predict_few<1>), grid, dim3(256), 0, s, m, tables, B, logp, ld);
+        else hipLaunchKernelGGL((k_predict_few<2>), grid, dim3(256), 0, s, m, tables, B, logp, ld);
+        return;
+    }
     const int64_t rows = (m.n_cats + 31ll) / 32;
-    int nt = B > 128 ? 8 : B > 64 ? 4 : B > 32 ? 2 : 1;
+    const bool exact = m.n_cats < 4096;
+    int nt = B > 128 && !exact ? 8 : B > 64 ? 4 : B > 32 ? 2 : 1;
     while (nt > 1 && rows * ((B + 32 * nt - 1) / (32 * nt)) < 1024) nt /= 2;
-#define PC_PREDICT(NT, WAVES, KC)                                                                                              \
-    if (nt == NT)                                                                                                              \
-        hipLaunchKernelGGL((k_predict<NT, WAVES, KC>), dim3((unsigned)((rows + WAVES - 1) / WAVES), (unsigned)((B + 32 * NT - 1) / (32 * NT))), \
-                           dim3(64 * WAVES), 0, s, m, tables, B, logp, ld)
-    PC_PREDICT(8, 8, 32);
-    PC_PREDICT(4, 4, 32);
-    PC_PREDICT(2, 4, 64);
-    PC_PREDICT(1, 4, 64);
+#define PC_PREDICT(NT, WAVES, SPLIT, KC, PLANES)                                                                               \
+    if (nt == NT && exact == (PLANES == 3)) {                                                                                  \
+        const dim3 grid((unsigned)((rows + WAVES / SPLIT - 1) / (WAVES / SPLIT)), (unsigned)((B + 32 * NT - 1) / (32 * NT)));  \
+        if (m.K % KC == 0) hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, true>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld); \
+        else hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, false>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld); \
+    }
+    PC_PREDICT(8, 8, 1, 32, 2)
+    PC_PREDICT(4, 4, 1, 32, 2)
+    PC_PREDICT(2, 4, 1, 32, 2)
+    PC_PREDICT(1, 4, 4, 32, 2)
+    PC_PREDICT(4, 4, 1, 32, 3)
+    PC_PREDICT(2, 4, 1, 32, 3)
+    PC_PREDICT(1, 4, 4, 32, 3)
 #undef PC_PREDICT
 }
 
@@ -282,6 +461,7 @@ static pc_status check_mixture(const pc_mixture *m, const float *tables, int32_t
         return fail(PC_ERR_ARG, "n_blocks, n_cats, n_tables and n_rows must be positive");
     if (B < 1) return fail(PC_ERR_ARG, "B must be positive");
     if (B > PC_MAX_BATCH) return fail(PC_ERR_TOO_LARGE, "more than PC_MAX_BATCH samples in one call");
+    if (m->n_rows < m->K) return fail(PC_ERR_ARG, "weights have fewer rows than a block");
     if (m->stride < B) return fail(PC_ERR_ARG, "stride is smaller than B");
     if ((int64_t)m->n_blocks * m->K > 1 << 30) return fail(PC_ERR_TOO_LARGE, "more than 2^30 states");
     if (m->n_cats > 1 << 29) return fail(PC_ERR_TOO_LARGE, "more than 2^29 categories");        // a grid has fewer than 2^32 threads along x
