@@ -372,50 +372,150 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
 }
 
 // g / p of one sample and category; p = 0 adds nothing
-__device__ inline float flow_ratio(float logp, float g) { return logp < kLogFltMin - 1e-3f ? 0.0f : g * expf(-logp); }
+__device__ inline float flow_ratio(float logp, float g) { return logp < kLogFltMin - 1e-3f || g == 0.0f ? 0.0f : g * expf(-logp); }
 
-// 64 categories x 64 nodes of a table a workgroup, the samples of all blocks of that table in steps of 16.  The table's first
-// block does the work, so that each entry has one writer.  Any K.
-__global__ __launch_bounds__(256) void k_predict_flow_any(const pc_mixture m, const float *__restrict__ tables, int32_t B,
-                                                          const float *__restrict__ logp, int64_t lp_ld, const float *__restrict__ dlogp,
-                                                          int64_t dl_ld, float scale, int32_t accumulate, float *__restrict__ flow)
+// Table flows.  A workgroup owns a tile of categories x columns, a column being a node of a block; the samples are added up 32 at a time
+// from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six products (the terms of a
+// flow have either sign and are few, so nothing averages out).  A wave holds IT x IT squares of 32 x 32 sums.  Bound by reading the tables
+// and writing their flows, which the waves of a CU's other workgroup cover with products: so one buffer, two barriers a step, two
+// workgroups a CU.  A table named by several blocks is the first one's: its column adds up all their weights, the others' columns do nothing,
+// so every entry has one writer.  The workgroups of a category tile follow one another on one XCD, whose cache keeps its g / p.
+template <int CW, int NW, int IT>
+__global__ __launch_bounds__(64 * CW * NW, IT == 2 ? 4 : 2) void k_predict_flow(const pc_mixture m, const float *__restrict__ tables, int32_t B,
+                                                                               const float *__restrict__ logp, int64_t lp_ld,
+                                                                               const float *__restrict__ dlogp, int64_t dl_ld, float scale,
+                                                                               int32_t accumulate, float *__restrict__ flow)
 {
-    __shared__ float rs[16][68], ws[16][68];
-    const int k_tiles = (m.K + 63) / 64;
-    const int c0 = blockIdx.x * 64, j0 = blockIdx.y / k_tiles, k0 = blockIdx.y % k_tiles * 64;
-    const int tk = threadIdx.x % 16 * 4, tc = threadIdx.x / 16 * 4;
-    const MixBlock mine = mix_block(m, j0);
-    if (mine.row < 0) return;
-    for (int j = 0; j < j0; ++j)
-        if (mix_block(m, j).table == mine.table) return;
-    float acc[4][4] = {};
-    for (int j = j0; j < m.n_blocks; ++j) {
-        const MixBlock blk = mix_block(m, j);
-        if (blk.table != mine.table) continue;
-        for (int b0 = 0; b0 < B; b0 += 16) {
-            for (int i = 0; i < 4; ++i) {
-                const int b = threadIdx.x / 64 + 4 * i, c = threadIdx.x % 64;
-                const bool on = b0 + b < B && c0 + c < m.n_cats;
-                rs[b][c] = on ? flow_ratio(logp[(int64_t)(b0 + b) * lp_ld + c0 + c], dlogp[(int64_t)(b0 + b) * dl_ld + c0 + c]) : 0.0f;
+    constexpr int TH = 64 * CW * NW, TC = 32 * IT * CW, TN = 32 * IT * NW, NP = TN + 2;   // two more: the four groups of a column lie in other banks
+    __shared__ uint4 rs[3][4][TC], ws[3][4][NP];      // [plane][8 samples][category or column]
+    __shared__ int64_t w_at[TN], o_at[TN];            // first weight of a column, -1: none; its place in the flows for category 0
+    __shared__ int32_t more[TN];                      // the column's table has further blocks
+    const int H = m.n_blocks * m.K, n_tiles = (H + TN - 1) / TN, q = blockIdx.x / 8;
+    const int64_t c0 = ((int64_t)(q / n_tiles) * 8 + blockIdx.x % 8) * TC;
+    const int n0 = q % n_tiles * TN;
+    if (c0 >= m.n_cats) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5, cw = wave / NW * 32 * IT, nw = wave % NW * 32 * IT;
+    const bool vec = m.stride % 4 == 0 && ((uintptr_t)m.weights & 15) == 0;
+    for (int i = threadIdx.x; i < TN; i += TH) {
+        const int n = n0 + i, j = n / m.K;
+        const MixBlock blk = n < H ? mix_block(m, j) : MixBlock{-1, -1};
+        bool mine = blk.row >= 0, again = false;
+        if (m.table && mine)
+            for (int o = 0; o < m.n_blocks; ++o)
+                if (o != j && m.table[o] == blk.table && mix_block(m, o).row >= 0) {
+                    if (o < j) mine = false;
+                    else again = true;
+                }
+        w_at[i] = mine ? (blk.row + n % m.K) * m.stride : -1;
+        o_at[i] = (int64_t)blk.table * m.n_cats * m.K + n % m.K;
+        more[i] = again;
+    }
+    floatx16 acc[IT][IT];
+#pragma unroll
+    for (int i = 0; i < IT; ++i)
+#pragma unroll
+        for (int k = 0; k < IT; ++k)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.0f;
+    // the eight weights of a row that begin with sample b
+    auto eight = [&](const float *row, int b, float (&x)[8]) {
+        if (vec && b + 8 <= B) {
+            const float4 u = *reinterpret_cast<const float4 *>(row + b), v = *reinterpret_cast<const float4 *>(row + b + 4);
+            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = b + i < B ? row[b + i] : 0.0f;
+        }
+    };
+    for (int b0 = 0; b0 < B; b0 += 32) {
+        __syncthreads();
+        for (int task = threadIdx.x; task < TC * 4; task += TH) {
+            const int c = task % TC, g = task / TC;
+            float x[8];
+            uint4 pl[3];
+            const float *lp = logp + (b0 + 8 * g) * lp_ld + c0 + c, *dl = dlogp + (b0 + 8 * g) * dl_ld + c0 + c;
+            const bool on = c0 + c < m.n_cats;
+            float l[8], d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool in = on && b0 + 8 * g + i < B;
+                l[i] = in ? lp[i * lp_ld] : 0.0f;
+                d[i] = in ? dl[i * dl_ld] : 0.0f;
             }
-            for (int i = 0; i < 4; ++i) {
-                const int b = threadIdx.x % 16, k = threadIdx.x / 16 + 16 * i;
-                ws[b][k] = b0 + b < B && k0 + k < m.K ? m.weights[(blk.row + k0 + k) * m.stride + b0 + b] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = flow_ratio(l[i], d[i]);
+            split8(x, pl);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) rs[p][g][c] = pl[p];
+        }
+        for (int task = threadIdx.x; task < TN * 4; task += TH) {
+            const int n = task / 4, g = task % 4, b = b0 + 8 * g;       // four lanes read 32 samples of a row
+            float x[8] = {};
+            uint4 pl[3];
+            if (w_at[n] >= 0) {
+                eight(m.weights + w_at[n], b, x);
+                if (more[n])
+                    for (int o = (n0 + n) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
+                        const MixBlock blk = mix_block(m, o);
+                        if (blk.row < 0 || blk.table != t) continue;
+                        float y[8];
+                        eight(m.weights + (blk.row + (n0 + n) % m.K) * m.stride, b, y);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] += y[i];
+                    }
             }
-            __syncthreads();
-            for (int b = 0; b < 16; ++b)
-                for (int i = 0; i < 4; ++i)
-                    for (int k = 0; k < 4; ++k) acc[i][k] += rs[b][tc + i] * ws[b][tk + k];
-            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= kUp;
+            split8(x, pl);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) ws[p][g][n] = pl[p];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            uint4 rp[IT][3];
+#pragma unroll
+            for (int i = 0; i < IT; ++i)
+#pragma unroll
+                for (int p = 0; p < 3; ++p) rp[i][p] = rs[p][2 * s + half][cw + 32 * i + col];
+#pragma unroll
+            for (int k = 0; k < IT; ++k) {
+                uint4 wp[3];
+#pragma unroll
+                for (int p = 0; p < 3; ++p) wp[p] = ws[p][2 * s + half][nw + 32 * k + col];
+#pragma unroll
+                for (int sum = 2; sum >= 0; --sum)     // the small products first
+#pragma unroll
+                    for (int p = sum; p >= 0; --p)
+#pragma unroll
+                        for (int i = 0; i < IT; ++i) acc[i][k] = mfma(rp[i][p], wp[sum - p], acc[i][k]);
+            }
         }
     }
-    for (int i = 0; i < 4; ++i)
-        for (int k = 0; k < 4; ++k)
-            if (c0 + tc + i < m.n_cats && k0 + tk + k < m.K) {
-                const int64_t at = ((int64_t)mine.table * m.n_cats + c0 + tc + i) * m.K + k0 + tk + k;
-                const float v = scale * (tables[at] * acc[i][k]);
-                flow[at] = accumulate ? flow[at] + v : v;
+#pragma unroll
+    for (int k = 0; k < IT; ++k) {
+        const int n = nw + 32 * k + col;
+        if (w_at[n] < 0) continue;
+        const int64_t at0 = o_at[n] + (c0 + cw + 4 * half) * m.K;
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            float t[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int c = 32 * i + 8 * (e / 4) + e % 4;
+                t[e] = c0 + cw + 4 * half + c < m.n_cats ? tables[at0 + (int64_t)c * m.K] : 0.0f;
             }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int c = 32 * i + 8 * (e / 4) + e % 4;
+                if (c0 + cw + 4 * half + c < m.n_cats) {
+                    float *out = flow + at0 + (int64_t)c * m.K;
+                    const float v = scale * (t[e] * (acc[i][k][e] * kDown));
+                    *out = accumulate ? *out + v : v;
+                }
+            }
+        }
+    }
 }
 
 // One or two samples of many categories: no matrix cores (4096 states x 50257 at one sample: 171 us against 211 with them, at four 212 against 200),
@@ -504,11 +604,18 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     if (logp_ld < m->n_cats || dlogp_ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4) || !aligned_to(dlogp, 4)) return fail(PC_ERR_ARG, "logp and dlogp must be 4-byte aligned");
     if (!aligned_to(table_flow, 16)) return fail(PC_ERR_ARG, "table_flow must be 16-byte aligned");
-    const int64_t rows = (int64_t)m->n_blocks * ((m->K + 63) / 64);
-    if (rows > 65535) return fail(PC_ERR_TOO_LARGE, "more than 65535 blocks in a mixture");
-    const dim3 grid((unsigned)((m->n_cats + 63ll) / 64), (unsigned)rows);
-    hipLaunchKernelGGL(k_predict_flow_any, grid, dim3(256), 0, (hipStream_t)stream, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale,
-                       accumulate, table_flow);
+    // large tiles where they give every CU a workgroup
+    const int64_t H = (int64_t)m->n_blocks * m->K, large = ((m->n_cats + 127ll) / 128) * ((H + 255) / 256);
+    const bool big = large >= 256;
+    const int64_t tc = big ? 128 : 64, tn = big ? 256 : 64, blocks = ((m->n_cats + tc - 1) / tc + 7) / 8 * 8 * ((H + tn - 1) / tn);
+    if (blocks * 512 > UINT32_MAX) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of flows");
+    const hipStream_t s = (hipStream_t)stream;
+    if (big)
+        hipLaunchKernelGGL((k_predict_flow<2, 4, 2>), dim3((unsigned)blocks), dim3(512), 0, s, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale, accumulate,
+                           table_flow);
+    else
+        hipLaunchKernelGGL((k_predict_flow<2, 2, 1>), dim3((unsigned)blocks), dim3(256), 0, s, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale, accumulate,
+                           table_flow);
     return launched();
 }
 
