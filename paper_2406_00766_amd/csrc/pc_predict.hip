@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "pc_internal.h"
 #include "pc_rows.h"
@@ -371,149 +372,284 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
     }
 }
 
-// g / p of one sample and category; p = 0 adds nothing
-__device__ inline float flow_ratio(float logp, float g) { return logp < kLogFltMin - 1e-3f || g == 0.0f ? 0.0f : g * expf(-logp); }
-
-// Table flows.  A workgroup owns a tile of categories x columns, a column being a node of a block; the samples are added up 32 at a time
-// from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six products (the terms of a
-// flow have either sign and are few, so nothing averages out).  A wave holds IT x IT squares of 32 x 32 sums.  Bound by reading the tables
-// and writing their flows, which the waves of a CU's other workgroup cover with products: so one buffer, two barriers a step, two
-// workgroups a CU.  A table named by several blocks is the first one's: its column adds up all their weights, the others' columns do nothing,
-// so every entry has one writer.  The workgroups of a category tile follow one another on one XCD, whose cache keeps its g / p.
-template <int CW, int NW, int IT>
-__global__ __launch_bounds__(64 * CW * NW, IT == 2 ? 4 : 2) void k_predict_flow(const pc_mixture m, const float *__restrict__ tables, int32_t B,
-                                                                               const float *__restrict__ logp, int64_t lp_ld,
-                                                                               const float *__restrict__ dlogp, int64_t dl_ld, float scale,
-                                                                               int32_t accumulate, float *__restrict__ flow)
+// g / p of one sample and category; p = 0 adds nothing.  exp(-logp) as 2^t times what t = -logp log2(e), rounded, leaves out: good to 2^-23 over the
+// whole range, for half the instructions of expf.
+__device__ inline float flow_ratio(float logp, float g)
 {
-    constexpr int TH = 64 * CW * NW, TC = 32 * IT * CW, TN = 32 * IT * NW, NP = TN + 2;   // two more: the four groups of a column lie in other banks
-    __shared__ uint4 rs[3][4][TC], ws[3][4][NP];      // [plane][8 samples][category or column]
+    constexpr float kLog2e = 1.44269504f, kRest = 1.92596299e-8f, kLn2 = 0.693147181f;    // log2(e) = kLog2e + kRest
+    const float t = -logp * kLog2e, rest = fmaf(-logp, kRest, fmaf(-logp, kLog2e, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return logp < kLogFltMin - 1e-3f ? 0.0f : g * fmaf(e, rest * kLn2, e);
+}
+
+// Column n of the flows: its first weight (-1: none, or another block's column does its table's work), its place in the flows for category 0,
+// and whether its table has further blocks.
+__device__ inline void flow_column(const pc_mixture &m, int n, int64_t &w_at, int64_t &o_at, int32_t &more)
+{
+    const int j = n / m.K;
+    const MixBlock blk = j < m.n_blocks ? mix_block(m, j) : MixBlock{-1, -1};
+    bool mine = blk.row >= 0, again = false;
+    if (m.table && mine)
+        for (int o = 0; o < m.n_blocks; ++o)
+            if (o != j && m.table[o] == blk.table && mix_block(m, o).row >= 0) {
+                if (o < j) mine = false;
+                else again = true;
+            }
+    w_at = mine ? (blk.row + n % m.K) * m.stride : -1;
+    o_at = blk.row >= 0 ? (int64_t)blk.table * m.n_cats * m.K + n % m.K : 0;      // a place that exists
+    more = again;
+}
+__device__ inline bool aligned_weights(const pc_mixture &m) { return m.stride % 4 == 0 && ((uintptr_t)m.weights & 15) == 0; }
+
+// Table flows.  A workgroup of 2 x 2 waves owns a tile of 64 IC categories x 64 IN columns, a column being a node of a block.  The samples are
+// added up 16 at a time from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six
+// products (the terms of a flow have either sign and are few, so that nothing averages out; the fp32 matrix instructions took longer:
+// 4096 states x 50257, B = 256 1372 us).  While a step is multiplied the next one's operands are split and staged and the one after is on its
+// way.  Bound by the matrix cores' sustained rate from some 150 samples on, before by reading the tables and writing their flows, which the
+// products of a CU's other workgroup cover.
+// SCAN: samples whose g is zero for all of the tile's categories are left out (targets of a few categories a sample: an EM step), except
+// where the first 32 of kSegment samples show that few are.
+// LISTS: a table named by several blocks is the first one's: its column adds up all their weights, the others' columns do nothing, so every entry has
+// one writer.  The workgroups of a category tile follow one another on one XCD, whose cache keeps its g / p.
+constexpr int kSegment = 512;
+template <int IC, int IN, bool SCAN, bool LISTS>
+__global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_flow(const pc_mixture m, const float *__restrict__ tables, int32_t B, const float *__restrict__ logp,
+                                                         int64_t lp_ld, const float *__restrict__ dlogp, int64_t dl_ld, float scale, int32_t accumulate,
+                                                         float *__restrict__ flow)
+{
+    constexpr int TH = 256, WAVES = 4, TC = 64 * IC, TN = 64 * IN, NP = TN + 4;   // four more: the two groups of a column lie in other banks
+    __shared__ uint4 rs[2][3][2][TC], ws[2][3][2][NP];                            // [buffer][plane][8 samples][category or column]
     __shared__ int64_t w_at[TN], o_at[TN];            // first weight of a column, -1: none; its place in the flows for category 0
     __shared__ int32_t more[TN];                      // the column's table has further blocks
+    __shared__ uint16_t list[SCAN ? kSegment : 1];    // samples of the segment that count
+    __shared__ uint8_t counts[SCAN ? kSegment : 1];
+    __shared__ int32_t n_list;
     const int H = m.n_blocks * m.K, n_tiles = (H + TN - 1) / TN, q = blockIdx.x / 8;
     const int64_t c0 = ((int64_t)(q / n_tiles) * 8 + blockIdx.x % 8) * TC;
     const int n0 = q % n_tiles * TN;
     if (c0 >= m.n_cats) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5, cw = wave / NW * 32 * IT, nw = wave % NW * 32 * IT;
-    const bool vec = m.stride % 4 == 0 && ((uintptr_t)m.weights & 15) == 0;
-    for (int i = threadIdx.x; i < TN; i += TH) {
-        const int n = n0 + i, j = n / m.K;
-        const MixBlock blk = n < H ? mix_block(m, j) : MixBlock{-1, -1};
-        bool mine = blk.row >= 0, again = false;
-        if (m.table && mine)
-            for (int o = 0; o < m.n_blocks; ++o)
-                if (o != j && m.table[o] == blk.table && mix_block(m, o).row >= 0) {
-                    if (o < j) mine = false;
-                    else again = true;
-                }
-        w_at[i] = mine ? (blk.row + n % m.K) * m.stride : -1;
-        o_at[i] = (int64_t)blk.table * m.n_cats * m.K + n % m.K;
-        more[i] = again;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+    const int cw = wave / 2 * 32 * IC, nw = wave % 2 * 32 * IN;
+    const bool vec = aligned_weights(m);
+    for (int i = threadIdx.x; i < TN; i += TH) flow_column(m, n0 + i, w_at[i], o_at[i], more[i]);
+    __syncthreads();
+    // What a thread stages a step: eight samples of a category (the group of samples is the wave's), and of a column (two lanes read 16 samples
+    // of a row).  Categories behind the last and columns without weights repeat others: their sums are not stored.
+    constexpr int WT = IN == 4 ? 2 : 1;               // columns of a thread
+    static_assert((IC == 2 && IN >= 2) || (IC == 1 && IN == 1), "the dealing below");
+    const bool of_ratios = IC == 2 || wave < 2, of_weights = IC == 2 || wave >= 2;
+    const int r_group = IC == 2 ? wave / 2 : wave % 2, r_cat = IC == 2 ? threadIdx.x % TC : lane, w_group = lane % 2;
+    const int64_t cat = min(c0 + r_cat, (int64_t)m.n_cats - 1);
+    int w_col[WT];
+    const float *w_row[WT];
+    bool w_more = false;
+#pragma unroll
+    for (int f = 0; f < WT; ++f) {
+        w_col[f] = threadIdx.x % (IC == 2 ? TH : TH / 2) / 2 + f * (TH / 2);
+        w_row[f] = m.weights + max(w_at[w_col[f]], (int64_t)0);
+        w_more |= w_at[w_col[f]] >= 0 && more[w_col[f]];
     }
-    floatx16 acc[IT][IT];
+    floatx16 acc[IC][IN];
 #pragma unroll
-    for (int i = 0; i < IT; ++i)
+    for (int i = 0; i < IC; ++i)
 #pragma unroll
-        for (int k = 0; k < IT; ++k)
+        for (int k = 0; k < IN; ++k)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.0f;
-    // the eight weights of a row that begin with sample b
-    auto eight = [&](const float *row, int b, float (&x)[8]) {
-        if (vec && b + 8 <= B) {
-            const float4 u = *reinterpret_cast<const float4 *>(row + b), v = *reinterpret_cast<const float4 *>(row + b + 4);
-            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-        } else {
+    bool none = true;                                  // no sample counts for this tile
+    for (int s0 = 0; s0 < B; s0 += SCAN ? kSegment : B) {
+        const int here = SCAN ? min(kSegment, B - s0) : B;
+        bool all = true;
+        if (SCAN) {
+            // which samples count: 32 at a time, all categories of the tile, a wave per sample
+            auto look = [&](int from, int to, auto at_once) {
+                constexpr int AT = decltype(at_once)::value;
+                for (int b0 = from + wave * AT; b0 < to; b0 += WAVES * AT) {
+                    float g[AT][IC];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = b + i < B ? row[b + i] : 0.0f;
+                    for (int e = 0; e < AT; ++e)
+#pragma unroll
+                        for (int i = 0; i < IC; ++i)
+                            g[e][i] = dlogp[(s0 + min(b0 + e, to - 1)) * dl_ld + min(c0 + lane + 64 * i, (int64_t)m.n_cats - 1)];
+#pragma unroll
+                    for (int e = 0; e < AT; ++e) {
+                        bool any = false;
+#pragma unroll
+                        for (int i = 0; i < IC; ++i) any |= g[e][i] != 0.0f;
+                        const bool on = __ballot(any) != 0;
+                        if (lane == 0 && b0 + e < to) counts[b0 + e] = on;
+                    }
+                }
+            };
+            auto compact = [&](int to) {               // one wave
+                int n = 0;
+                for (int b = 0; b < to; b += 64) {
+                    const bool on = b + lane < to && counts[b + lane];
+                    const uint64_t those = __ballot(on);
+                    if (on) list[n + __popcll(those & ((1ull << lane) - 1))] = (uint16_t)(b + lane);
+                    n += __popcll(those);
+                }
+                if (lane == 0) n_list = n;
+            };
+            const int few = min(here, 32);
+            __syncthreads();
+            look(0, few, std::integral_constant<int, 8>{});
+            __syncthreads();
+            if (wave == 0) compact(few);
+            __syncthreads();
+            all = n_list * 4 > few * 3;
+            __syncthreads();
+            if (!all && here > few) {
+                look(few, here, std::integral_constant<int, 32>{});
+                __syncthreads();
+                if (wave == 0) compact(here);
+                __syncthreads();
+            }
         }
-    };
-    for (int b0 = 0; b0 < B; b0 += 32) {
-        __syncthreads();
-        for (int task = threadIdx.x; task < TC * 4; task += TH) {
-            const int c = task % TC, g = task / TC;
+        const int n_samples = all ? here : n_list;
+        if (n_samples == 0) continue;
+        none = false;
+        auto sample = [&](int i) { return s0 + (!SCAN || all ? i : list[i]); };
+        float l[8], d[8], w[WT][8];
+        auto fetch_ratios = [&](int i0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t at = __builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * r_group + e, n_samples - 1)));
+                l[e] = (logp + at * lp_ld)[cat];
+                d[e] = (dlogp + at * dl_ld)[cat];
+            }
+        };
+        auto stage_ratios = [&](int i0, int buf) {
             float x[8];
             uint4 pl[3];
-            const float *lp = logp + (b0 + 8 * g) * lp_ld + c0 + c, *dl = dlogp + (b0 + 8 * g) * dl_ld + c0 + c;
-            const bool on = c0 + c < m.n_cats;
-            float l[8], d[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool in = on && b0 + 8 * g + i < B;
-                l[i] = in ? lp[i * lp_ld] : 0.0f;
-                d[i] = in ? dl[i * dl_ld] : 0.0f;
-            }
+            for (int e = 0; e < 8; ++e) x[e] = flow_ratio(l[e], d[e]);
+            if (i0 + 16 > n_samples)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = flow_ratio(l[i], d[i]);
+                for (int e = 0; e < 8; ++e) x[e] = i0 + 8 * r_group + e < n_samples ? x[e] : 0.0f;
             split8(x, pl);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) rs[p][g][c] = pl[p];
-        }
-        for (int task = threadIdx.x; task < TN * 4; task += TH) {
-            const int n = task / 4, g = task % 4, b = b0 + 8 * g;       // four lanes read 32 samples of a row
-            float x[8] = {};
+            for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = pl[p];
+        };
+        auto eight = [&](const float *row, int i0, float (&x)[8]) {
+            const int i = i0 + 8 * w_group;
+            if (all && vec && i0 + 16 <= n_samples) {
+                const float4 u = *reinterpret_cast<const float4 *>(row + s0 + i), v = *reinterpret_cast<const float4 *>(row + s0 + i + 4);
+                x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = row[sample(min(i + e, n_samples - 1))];
+            }
+        };
+        auto fetch_weights = [&](int i0, int f) {
+            eight(w_row[f], i0, w[f]);
+            if (LISTS && w_more && w_at[w_col[f]] >= 0 && more[w_col[f]])
+                for (int o = (n0 + w_col[f]) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
+                    const MixBlock blk = mix_block(m, o);
+                    if (blk.row < 0 || blk.table != t) continue;
+                    float y[8];
+                    eight(m.weights + (blk.row + (n0 + w_col[f]) % m.K) * m.stride, i0, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[f][e] += y[e];
+                }
+        };
+        auto stage_weights = [&](int i0, int buf, int f) {
+            float x[8];
             uint4 pl[3];
-            if (w_at[n] >= 0) {
-                eight(m.weights + w_at[n], b, x);
-                if (more[n])
-                    for (int o = (n0 + n) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
-                        const MixBlock blk = mix_block(m, o);
-                        if (blk.row < 0 || blk.table != t) continue;
-                        float y[8];
-                        eight(m.weights + (blk.row + (n0 + n) % m.K) * m.stride, b, y);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] += y[i];
-                    }
-            }
+            for (int e = 0; e < 8; ++e) x[e] = w[f][e] * kUp;
+            if (i0 + 16 > n_samples)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= kUp;
+                for (int e = 0; e < 8; ++e) x[e] = i0 + 8 * w_group + e < n_samples ? x[e] : 0.0f;
             split8(x, pl);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) ws[p][g][n] = pl[p];
-        }
+            for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col[f]] = pl[p];
+        };
+        __syncthreads();                               // the segment before is read
+        if (of_ratios) fetch_ratios(0);
+#pragma unroll
+        for (int f = 0; f < WT; ++f)
+            if (of_weights) fetch_weights(0, f);
+        if (of_ratios) { stage_ratios(0, 0); fetch_ratios(16); }
+#pragma unroll
+        for (int f = 0; f < WT; ++f)
+            if (of_weights) { stage_weights(0, 0, f); fetch_weights(16, f); }
         __syncthreads();
+        for (int i0 = 0, buf = 0; i0 < n_samples; i0 += 16, buf ^= 1) {
+            const bool next = i0 + 16 < n_samples;
+            uint4 rp[IC][3];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            uint4 rp[IT][3];
+            for (int i = 0; i < IC; ++i)
 #pragma unroll
-            for (int i = 0; i < IT; ++i)
+                for (int p = 0; p < 3; ++p) rp[i][p] = rs[buf][p][half][cw + 32 * i + col];
 #pragma unroll
-                for (int p = 0; p < 3; ++p) rp[i][p] = rs[p][2 * s + half][cw + 32 * i + col];
-#pragma unroll
-            for (int k = 0; k < IT; ++k) {
+            for (int k = 0; k < IN; ++k) {
                 uint4 wp[3];
 #pragma unroll
-                for (int p = 0; p < 3; ++p) wp[p] = ws[p][2 * s + half][nw + 32 * k + col];
+                for (int p = 0; p < 3; ++p) wp[p] = ws[buf][p][half][nw + 32 * k + col];
 #pragma unroll
                 for (int sum = 2; sum >= 0; --sum)     // the small products first
 #pragma unroll
                     for (int p = sum; p >= 0; --p)
 #pragma unroll
-                        for (int i = 0; i < IT; ++i) acc[i][k] = mfma(rp[i][p], wp[sum - p], acc[i][k]);
+                        for (int i = 0; i < IC; ++i) acc[i][k] = mfma(rp[i][p], wp[sum - p], acc[i][k]);
+                if (next && k < WT && of_weights) { stage_weights(i0 + 16, buf ^ 1, k); fetch_weights(i0 + 32, k); }
+                if (next && k == (IN == 4 ? 2 : IN - 1) && of_ratios) { stage_ratios(i0 + 16, buf ^ 1); fetch_ratios(i0 + 32); }
+                __builtin_amdgcn_sched_barrier(0);
             }
+            __syncthreads();
         }
     }
+    if (SCAN && none && accumulate) return;
+    // A whole tile of tables below 4 GiB: 32-bit offsets from addresses that all lanes share, a square's entries on their way while the one
+    // before is stored.  Else entry by entry.
+    auto finish = [&](auto add) {
+        constexpr bool ADD = decltype(add)::value;
+        float t[2][16];
+        auto offset = [&](int sq) { return (uint32_t)((o_at[nw + 32 * (sq / IC) + col] + (c0 + cw + 32 * (sq % IC) + 4 * half) * m.K) * 4); };
+        auto entry = [&](int e) { return (int64_t)(8 * (e / 4) + e % 4) * m.K * 4; };
+        auto fetch = [&](int sq) {
+            const uint32_t at = offset(sq);
+            if (SCAN && none) return;                  // the sums are zero
 #pragma unroll
-    for (int k = 0; k < IT; ++k) {
-        const int n = nw + 32 * k + col;
-        if (w_at[n] < 0) continue;
-        const int64_t at0 = o_at[n] + (c0 + cw + 4 * half) * m.K;
+            for (int e = 0; e < 16; ++e) t[sq & 1][e] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(tables) + entry(e) + at);
+        };
+        fetch(0);
 #pragma unroll
-        for (int i = 0; i < IT; ++i) {
-            float t[16];
+        for (int sq = 0; sq < IC * IN; ++sq) {
+            if (sq + 1 < IC * IN) fetch(sq + 1);
+            const uint32_t at = offset(sq);
+            if (w_at[nw + 32 * (sq / IC) + col] >= 0) {
+                float old[16];
+                if (ADD)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int c = 32 * i + 8 * (e / 4) + e % 4;
-                t[e] = c0 + cw + 4 * half + c < m.n_cats ? tables[at0 + (int64_t)c * m.K] : 0.0f;
-            }
+                    for (int e = 0; e < 16; ++e) old[e] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(flow) + entry(e) + at);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int c = 32 * i + 8 * (e / 4) + e % 4;
-                if (c0 + cw + 4 * half + c < m.n_cats) {
-                    float *out = flow + at0 + (int64_t)c * m.K;
-                    const float v = scale * (t[e] * (acc[i][k][e] * kDown));
-                    *out = accumulate ? *out + v : v;
+                for (int e = 0; e < 16; ++e) {
+                    const float v = SCAN && none ? 0.0f : scale * (t[sq & 1][e] * (acc[sq % IC][sq / IC][e] * kDown));
+                    *reinterpret_cast<float *>(reinterpret_cast<char *>(flow) + entry(e) + at) = ADD ? old[e] + v : v;
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (c0 + TC <= m.n_cats && (int64_t)m.n_tables * m.n_cats * m.K < 1ll << 30) {
+        if (accumulate) finish(std::true_type{});
+        else finish(std::false_type{});
+        return;
+    }
+#pragma unroll
+    for (int sq = 0; sq < IC * IN; ++sq) {
+        const int n = nw + 32 * (sq / IC) + col;
+        if (w_at[n] < 0) continue;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int64_t c = c0 + cw + 32 * (sq % IC) + 4 * half + 8 * (e / 4) + e % 4, at = o_at[n] + c * m.K;
+            if (c < m.n_cats) {
+                const float v = scale * (tables[at] * (acc[sq % IC][sq / IC][e] * kDown));
+                flow[at] = accumulate ? flow[at] + v : v;
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
@@ -604,18 +740,19 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     if (logp_ld < m->n_cats || dlogp_ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4) || !aligned_to(dlogp, 4)) return fail(PC_ERR_ARG, "logp and dlogp must be 4-byte aligned");
     if (!aligned_to(table_flow, 16)) return fail(PC_ERR_ARG, "table_flow must be 16-byte aligned");
-    // large tiles where they give every CU a workgroup
-    const int64_t H = (int64_t)m->n_blocks * m->K, large = ((m->n_cats + 127ll) / 128) * ((H + 255) / 256);
-    const bool big = large >= 256;
-    const int64_t tc = big ? 128 : 64, tn = big ? 256 : 64, blocks = ((m->n_cats + tc - 1) / tc + 7) / 8 * 8 * ((H + tn - 1) / tn);
-    if (blocks * 512 > UINT32_MAX) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of flows");
+    // Tiles: 128 x 256 for many samples, 128 x 128 for fewer (a third workgroup a CU reads and writes: 4096 states x 50257, B = 32 410 us against 466,
+    // B = 256 1161 against 981), where they give every CU two; else 64 x 64.  Looking for samples to leave out pays from some 128 on.
+    const int64_t H = (int64_t)m->n_blocks * m->K;
+    const auto tiles = [&](int64_t tc, int64_t tn) { return ((m->n_cats + tc - 1) / tc + 7) / 8 * 8 * ((H + tn - 1) / tn); };
     const hipStream_t s = (hipStream_t)stream;
-    if (big)
-        hipLaunchKernelGGL((k_predict_flow<2, 4, 2>), dim3((unsigned)blocks), dim3(512), 0, s, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale, accumulate,
-                           table_flow);
-    else
-        hipLaunchKernelGGL((k_predict_flow<2, 2, 1>), dim3((unsigned)blocks), dim3(256), 0, s, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale, accumulate,
-                           table_flow);
+    if (tiles(64, 64) > 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of flows");
+#define PC_FLOW(IC, IN, SCAN)                                                                                                              \
+    hipLaunchKernelGGL((m->table ? k_predict_flow<IC, IN, SCAN, true> : k_predict_flow<IC, IN, SCAN, false>), dim3((unsigned)tiles(64 * IC, 64 * IN)), dim3(256), 0, \
+                       s, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale, accumulate, table_flow)
+    if (tiles(128, 256) >= 512 && B >= 128) PC_FLOW(2, 4, true);
+    else if (tiles(128, 128) >= 512) PC_FLOW(2, 2, false);
+    else PC_FLOW(1, 1, false);
+#undef PC_FLOW
     return launched();
 }
 

@@ -64,7 +64,10 @@ def check_flow(got, want, bound, n):
 
 SIZES = [(1, 1, 1, 1), (1, 3, 2, 5), (2, 1, 7, 33), (7, 5, 65, 31), (16, 1, 64, 32), (16, 3, 129, 64), (24, 2, 31, 65), (32, 1, 300, 1),
          (32, 9, 33, 130), (33, 2, 70, 20), (48, 2, 260, 3), (64, 2, 256, 257), (64, 7, 1000, 77), (96, 1, 63, 128), (100, 3, 65, 16),
-         (127, 1, 127, 127), (128, 3, 517, 40), (128, 2, 5003, 1), (128, 1, 32, 513), (64, 1, 4099, 300)]
+         (127, 1, 127, 127), (128, 3, 517, 40), (128, 2, 5003, 1), (128, 1, 32, 513), (64, 1, 4099, 300),
+         # every tile shape of the rules: 64, 128 and 256 samples a wave, two planes and three, blocks shorter and longer than a chunk; flows by 128 x 128
+         (16, 4, 33000, 40), (20, 3, 32800, 100), (32, 4, 17000, 300), (48, 2, 33000, 65), (128, 1, 4000, 600), (20, 5, 4000, 1200), (100, 1, 3000, 1300),
+         (128, 4, 16500, 37), (64, 8, 16411, 2), (128, 16, 16411, 1), (33, 8, 17000, 70)]
 
 
 @pytest.mark.parametrize("K,nb,V,B", SIZES)
@@ -118,6 +121,39 @@ def test_block_lists_with_gaps_shared_tables_and_entries_out_of_range():
             continue
         ws = sum(full[a:a + K].astype(np.float64) for a in mine)
         check_flow(got[j], (ws @ r).T * t[j], (ws @ np.abs(r)).T * t[j], B * len(mine))
+
+
+@pytest.mark.parametrize("B,density", [(128, 0.0), (130, 0.002), (300, 0.01), (700, 0.002), (1100, 0.02), (256, 0.9)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_flows_of_targets_of_few_categories(B, density, shared):
+    """Gradients that are zero almost everywhere, in large tiles: samples are left out tile by tile; tables that two blocks share."""
+    K, nb, V = 32, 32, 16500                                # 128 x 256 tiles, 512 of them
+    print(f"case sparse flows B={B} density={density} shared={shared}", flush=True)
+    full, t = make(K, nb, V, B, 5 + B, extra_cols=B % 2)
+    rng = np.random.default_rng(B)
+    g = (-rng.random((B, V)) * (rng.random((B, V)) < density)).astype(np.float32)
+    g[:, 200:900] = 0.0
+    table = np.arange(nb, dtype=np.int32)
+    if shared:
+        table[5], table[9] = 2, 8
+    m = pcb.mixture(torch.from_numpy(full).cuda(), K, V, nb, table=torch.from_numpy(table).cuda() if shared else None, n_tables=nb)
+    p = exact_p(full, t, B, np.arange(nb) * K, table)
+    logp = np.log(p).astype(np.float32)
+    base = np.full(t.shape, 0.25, np.float32)
+    r = g / np.exp(logp.astype(np.float64))
+    f64 = full[:, :B].astype(np.float64)
+    w = np.zeros((nb, K, B))
+    for j in range(nb):
+        w[table[j]] += f64[j * K:(j + 1) * K]
+    sums = np.stack([(w[j] @ r).T for j in range(nb)]) * t
+    bound = np.stack([(w[j] @ np.abs(r)).T for j in range(nb)]) * t
+    for accumulate in (False, True):
+        flow = torch.from_numpy(base.copy()).cuda()
+        pcb.pc_predict_backward(m, torch.from_numpy(t).cuda(), B, torch.from_numpy(logp).cuda(), torch.from_numpy(g).cuda(), -1.0, flow, accumulate=accumulate)
+        got = flow.cpu().numpy().astype(np.float64)
+        used = np.isin(np.arange(nb), table)
+        assert np.all(got[~used] == 0.25)
+        check_flow(got[used], (-sums + (0.25 if accumulate else 0.0))[used], (bound + (0.25 if accumulate else 0.0))[used], 2 * B)
 
 
 def test_flows_are_the_gradient_with_respect_to_log_tables():
