@@ -13,25 +13,6 @@
 
 namespace pc {
 
-constexpr int kRowThreads = 256;
-
-// Sum / maximum over a workgroup of kRowThreads; every thread gets the result.
-template <typename F>
-__device__ inline float block_all(float v, float *lds, F op)
-{
-    for (int d = 32; d > 0; d >>= 1) v = op(v, __shfl_xor(v, d));
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < kRowThreads / 64; ++w) v = op(v, lds[w]);
-    return v;
-}
-__device__ inline float add2(float a, float b) { return a + b; }
-__device__ inline float max2(float a, float b) { return fmaxf(a, b); }
-// exp(a - m) of a running maximum m; nothing seen yet (-inf) counts as 0
-__device__ inline float exp_below(float a, float m, float inv_T) { return m == PC_NEG_INF_F ? 0.0f : expf((a - m) * inv_T); }
-
 struct DistillDev {                                   // pc_distill without its types
     int64_t rows, student_ld, ids_ld, teacher_ld;
     int32_t n_cats, top;
@@ -42,72 +23,163 @@ struct DistillDev {                                   // pc_distill without its 
     bool normalised;
 };
 
-// The list of a row: q and log q per entry, in registers of thread j mod kRowThreads; out of range or -inf: q = 0.
-constexpr int kListRegs = PC_MAX_TOP / kRowThreads;
-template <typename TT>
-__device__ inline void row_targets(const DistillDev &d, int64_t r, float *lds, int32_t (&id)[kListRegs], float (&q)[kListRegs], float (&logq)[kListRegs])
+__device__ inline float add2(float a, float b) { return a + b; }
+__device__ inline float max2(float a, float b) { return fmaxf(a, b); }
+template <typename F>
+__device__ inline float wave_all(float v, F op)
 {
-    const TT *teacher = (const TT *)d.teacher + r * d.teacher_ld;
-    const int32_t *ids = d.ids + r * d.ids_ld;
-    float m = PC_NEG_INF_F;
-    for (int i = 0; i < kListRegs; ++i) {
-        const int j = threadIdx.x + i * kRowThreads;
-        id[i] = -1;
-        logq[i] = PC_NEG_INF_F;
-        if (j < d.top) {
-            const int32_t c = ids[j];
-            if (c >= 0 && c < d.n_cats) { id[i] = c; logq[i] = to_f32(teacher[j]); }
-        }
-        m = max2(m, logq[i]);
-    }
-    float shift = 0.0f, base = 0.0f;
-    if (d.teacher_lse) {
-        base = d.teacher_lse[r];
-    } else {
-        shift = block_all(m, lds, max2);
-        if (shift == PC_NEG_INF_F) shift = 0.0f;      // nothing listed: every q is 0
-        float s = 0.0f;
-        for (int i = 0; i < kListRegs; ++i) s += expf((logq[i] - shift) * d.inv_T);
-        base = logf(block_all(s, lds, add2));
-    }
-    for (int i = 0; i < kListRegs; ++i) {
-        logq[i] = logq[i] == PC_NEG_INF_F ? PC_NEG_INF_F : (logq[i] - shift) * d.inv_T - base;
-        q[i] = expf(logq[i]);
-    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = op(v, __shfl_xor(v, d));
+    return v;
 }
 
-template <typename TS, typename TT>
-__global__ __launch_bounds__(kRowThreads) void k_distill_rows(const DistillDev d, float *__restrict__ loss, float *__restrict__ stats)
+// A row is worked on by WAVES waves of a workgroup.  Its list lies with the first of them where it has at most 64 entries (LONG = false: no
+// barriers), else with all of them, LIST entries a lane.
+constexpr int kShortList = 64;
+template <int WAVES, bool LONG>
+struct Group {
+    static constexpr int THREADS = 64 * WAVES, LIST = LONG ? PC_MAX_TOP / THREADS : 1;
+    static constexpr int ROWS = WAVES >= 4 ? 1 : 4 / WAVES;              // rows of a workgroup
+    static constexpr int BLOCK = THREADS * ROWS;
+    // over the lanes that have the list
+    template <typename F>
+    __device__ static inline float list_all(float v, float *lds, F op)
+    {
+        v = wave_all(v, op);
+        if (!LONG) return v;
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+        __syncthreads();
+        v = lds[0];
+        for (int w = 1; w < WAVES; ++w) v = op(v, lds[w]);
+        return v;
+    }
+};
+
+// The list of a row: category, q and log q of entry t + i * THREADS; out of range or -inf: q = 0.  Fetched first, made into
+// probabilities once the rest of the row is on its way.
+template <typename G, typename TT>
+struct List {
+    int32_t id[G::LIST];
+    float q[G::LIST], logq[G::LIST], norm;
+    __device__ inline void fetch(const DistillDev &d, int64_t r, int t)
+    {
+        const TT *teacher = (const TT *)d.teacher + r * d.teacher_ld;
+        const int32_t *ids = d.ids + r * d.ids_ld;
+        norm = d.teacher_lse ? d.teacher_lse[r] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < G::LIST; ++i) {
+            const int j = t + i * G::THREADS;
+            id[i] = j < d.top ? ids[j] : -1;
+            logq[i] = j < d.top ? to_f32(teacher[j]) : PC_NEG_INF_F;
+        }
+    }
+    __device__ inline void probabilities(const DistillDev &d, float *lds)
+    {
+        float m = PC_NEG_INF_F, shift = 0.0f;
+#pragma unroll
+        for (int i = 0; i < G::LIST; ++i) {
+            if (id[i] < 0 || id[i] >= d.n_cats) { id[i] = -1; logq[i] = PC_NEG_INF_F; }
+            m = max2(m, logq[i]);
+        }
+        if (!d.teacher_lse) {
+            shift = G::list_all(m, lds, max2);
+            if (shift == PC_NEG_INF_F) shift = 0.0f;  // nothing listed: every q is 0
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < G::LIST; ++i) s += expf((logq[i] - shift) * d.inv_T);
+            norm = logf(G::list_all(s, lds, add2));
+        }
+#pragma unroll
+        for (int i = 0; i < G::LIST; ++i) {
+            logq[i] = logq[i] == PC_NEG_INF_F ? PC_NEG_INF_F : (logq[i] - shift) * d.inv_T - norm;
+            q[i] = expf(logq[i]);
+        }
+    }
+};
+
+// Loss and statistics.  A row passes through registers once, kPacks x 16 bytes a lane at a time, the next ones on their way, with a running
+// maximum and sum per lane: bound by reading it.  Many rows: four waves a row (one where a row is a few packs), so that a CU's
+// other rows cover what follows a row's last load.  Few rows: sixteen.
+constexpr int kPacks = 4;
+template <typename TS, typename TT, int WAVES, bool LONG>
+__global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(const DistillDev d, float *__restrict__ loss, float *__restrict__ stats)
 {
-    __shared__ float lds[kRowThreads / 64];
-    for (int64_t r = blockIdx.x; r < d.rows; r += gridDim.x) {
+    using G = Group<WAVES, LONG>;
+    constexpr int N = Pack<TS>::N, TH = G::THREADS;
+    __shared__ float lds[WAVES], wave_m[WAVES], wave_s[WAVES];
+    const int t = threadIdx.x % TH, sub = threadIdx.x / TH;
+    for (int64_t r = (int64_t)blockIdx.x * G::ROWS + sub; r < d.rows; r += (int64_t)gridDim.x * G::ROWS) {
         const TS *z = (const TS *)d.student + r * d.student_ld;
+        const bool listing = LONG || t < 64;
+        List<G, TT> list;
+        if (listing) list.fetch(d, r, t);
         float m = PC_NEG_INF_F, s = 0.0f, log_s = 0.0f;
         if (!d.normalised) {
-            for (int c = threadIdx.x; c < d.n_cats; c += kRowThreads) {
-                const float v = to_f32(z[c]), above = max2(m, v);
-                s = s * exp_below(m, above, d.inv_T) + exp_below(v, above, d.inv_T);
-                if (v != v) s = v;
-                m = above;
+            // packs of the 16-byte grid; the first and last may be cut, their missing elements count as -inf
+            const int off = elements_off(z);
+            const TS *grid = z - off;
+            const int64_t end = off + (int64_t)d.n_cats, packs = (end + N - 1) / N;
+            float v[kPacks * N];
+            Pack<TS> ahead[kPacks];
+            auto fetch = [&](int64_t p0) {             // whole packs; a pack that is none or cut reads the first whole one that exists, or nothing
+#pragma unroll
+                for (int k = 0; k < kPacks; ++k) {
+                    const int64_t i = (p0 + t + k * TH) * N;
+                    if (i >= off && i + N <= end) ahead[k] = *reinterpret_cast<const Pack<TS> *>(__builtin_assume_aligned(grid + i, 16));
+                }
+            };
+            fetch(0);
+            for (int64_t p0 = 0; p0 < packs; p0 += kPacks * TH) {
+                const bool inner = p0 > 0 && (p0 + kPacks * TH) * N <= end;
+#pragma unroll
+                for (int k = 0; k < kPacks; ++k) {
+                    const int64_t i = (p0 + t + k * TH) * N;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[k * N + e] = to_f32(ahead[k].v[e]);
+                    if (!inner && !(i >= off && i + N <= end))
+#pragma unroll
+                        for (int e = 0; e < N; ++e) v[k * N + e] = i + e >= off && i + e < end ? to_f32(grid[i + e]) : PC_NEG_INF_F;
+                }
+                if (p0 + kPacks * TH < packs) fetch(p0 + kPacks * TH);
+                float top = v[0];
+#pragma unroll
+                for (int e = 1; e < kPacks * N; ++e) top = max2(top, v[e]);
+                if (top > m) { s *= exp2f((m - top) * (d.inv_T * PC_LOG2E_F)); m = top; }
+                const float at = m == PC_NEG_INF_F ? 0.0f : m, c = d.inv_T * PC_LOG2E_F;
+                float part = 0.0f;
+#pragma unroll
+                for (int e = 0; e < kPacks * N; ++e) part += __builtin_amdgcn_exp2f((v[e] - at) * c);
+                s += part;
             }
-            const float all = block_all(m, lds, max2);
-            s = block_all(s * exp_below(m, all, d.inv_T), lds, add2);
+            auto below = [&](float a, float b) { return a == PC_NEG_INF_F ? 1.0f : exp2f((a - b) * (d.inv_T * PC_LOG2E_F)); };   // (s is 0, or NaN)
+            float all = wave_all(m, max2);
+            s = wave_all(s * below(m, all), add2);
+            if (WAVES > 1) {
+                __syncthreads();                       // the row before is read
+                if (t % 64 == 0) { wave_m[t / 64] = all; wave_s[t / 64] = s; }
+                __syncthreads();
+                for (int w = 0; w < WAVES; ++w) all = max2(all, wave_m[w]);
+                s = 0.0f;
+                for (int w = 0; w < WAVES; ++w) s += wave_s[w] * below(wave_m[w], all);
+            }
             m = s != s && all < __builtin_inff() ? s : all;   // a row with a NaN has no maximum, not even where all else is -inf
             log_s = logf(s);
         } else {
             m = 0.0f;
         }
-        int32_t id[kListRegs];
-        float q[kListRegs], logq[kListRegs], part = 0.0f;
-        row_targets<TT>(d, r, lds, id, q, logq);
-        for (int i = 0; i < kListRegs; ++i)
-            if (id[i] >= 0 && !(q[i] == 0.0f)) {
-                const float v = to_f32(z[id[i]]);
+        if (!listing) continue;
+        list.probabilities(d, lds);
+        float part = 0.0f;
+#pragma unroll
+        for (int i = 0; i < G::LIST; ++i)
+            if (list.id[i] >= 0 && !(list.q[i] == 0.0f)) {
+                const float v = to_f32(z[list.id[i]]);
                 const float logp = d.normalised ? v : m == PC_NEG_INF_F ? m : (v - m) * d.inv_T - log_s;
-                part += q[i] * (logq[i] - logp);
+                part += list.q[i] * (list.logq[i] - logp);
             }
-        part = block_all(part, lds, add2);
-        if (threadIdx.x == 0) {
+        part = G::list_all(part, lds, add2);
+        if (t == 0) {
             loss[r] = part;
             stats[2 * r] = m;
             stats[2 * r + 1] = log_s;
@@ -115,50 +187,97 @@ __global__ __launch_bounds__(kRowThreads) void k_distill_rows(const DistillDev d
     }
 }
 
-// The listed entries are written after a barrier over what the row's dense part put there.
-template <typename TS, typename TT>
-__global__ __launch_bounds__(kRowThreads) void k_distill_grad(const DistillDev d, const float *__restrict__ stats, const float *__restrict__ dloss,
-                                                              float scale, void *dstudent, int64_t out_ld)
+// Gradient.  The listed categories' values are made first (from the row itself where the gradient replaces it), then the dense part is
+// written in packs of the output's 16-byte grid, then, behind a barrier, the listed ones over it.
+template <typename TS, typename TT, int WAVES, bool LONG>
+__global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(const DistillDev d, const float *__restrict__ stats,
+                                                                               const float *__restrict__ dloss, float scale, void *dstudent, int64_t out_ld)
 {
-    __shared__ float lds[kRowThreads / 64];
-    __shared__ int32_t ids[PC_MAX_TOP];
-    __shared__ float qs[PC_MAX_TOP];
-    for (int64_t r = blockIdx.x; r < d.rows; r += gridDim.x) {
+    using G = Group<WAVES, LONG>;
+    constexpr int N = Pack<TS>::N, TH = G::THREADS;
+    __shared__ float lds[WAVES], shared_Q[G::ROWS];
+    __shared__ int32_t ids[LONG ? PC_MAX_TOP : 1];
+    __shared__ float qs[LONG ? PC_MAX_TOP : 1];
+    const int t = threadIdx.x % TH, sub = threadIdx.x / TH;
+    const bool listing = LONG || t < 64;
+    for (int64_t r = (int64_t)blockIdx.x * G::ROWS + sub; r < d.rows; r += (int64_t)gridDim.x * G::ROWS) {
         const TS *z = (const TS *)d.student + r * d.student_ld;
         TS *out = (TS *)dstudent + r * out_ld;
         const float g = (dloss ? scale * dloss[r] : scale) * d.inv_T;
-        int32_t id[kListRegs];
-        float q[kListRegs], logq[kListRegs], at[kListRegs], Q = 0.0f;
-        row_targets<TT>(d, r, lds, id, q, logq);
-        __syncthreads();
-        for (int i = 0; i < kListRegs; ++i) {
-            const int j = threadIdx.x + i * kRowThreads;
-            Q += q[i];
-            at[i] = id[i] >= 0 && !d.normalised ? to_f32(z[id[i]]) : 0.0f;
-            if (j < d.top) { ids[j] = id[i]; qs[j] = q[i]; }
+        const float m = stats[2 * r], log_s = stats[2 * r + 1], c = d.inv_T * PC_LOG2E_F;
+        List<G, TT> list;
+        float at[G::LIST], Q = 0.0f;
+        if (listing) {
+            list.fetch(d, r, t);
+            list.probabilities(d, lds);
+#pragma unroll
+            for (int i = 0; i < G::LIST; ++i) {
+                Q += list.q[i];
+                at[i] = list.id[i] >= 0 && !d.normalised ? to_f32(z[list.id[i]]) : 0.0f;
+            }
+            Q = G::list_all(Q, lds, add2);
+            if (LONG)
+#pragma unroll
+                for (int i = 0; i < G::LIST; ++i)
+                    if (t + i * TH < d.top) { ids[t + i * TH] = list.id[i]; qs[t + i * TH] = list.q[i]; }
         }
-        Q = block_all(Q, lds, add2);
-        const bool none = g == 0.0f || Q == 0.0f;
-        const float m = stats[2 * r], log_s = stats[2 * r + 1];
-        auto dense = [&](float v) {
-            return none || d.normalised || m == PC_NEG_INF_F ? 0.0f : expf((v - m) * d.inv_T - log_s) * Q;
-        };
-        __syncthreads();
-        if (none || d.normalised)
-            for (int c = threadIdx.x; c < d.n_cats; c += kRowThreads) out[c] = from_f32<TS>(0.0f);
-        else
-            for (int c = threadIdx.x; c < d.n_cats; c += kRowThreads) out[c] = from_f32<TS>(g * dense(to_f32(z[c])));
-        __syncthreads();
-        if (none) continue;
-        for (int i = 0; i < kListRegs; ++i) {
-            const int j = threadIdx.x + i * kRowThreads;
-            if (id[i] < 0) continue;
-            bool first = true;
-            float sum = 0.0f;                         // a category listed more than once: its first entry writes for all
-            for (int k = 0; k < d.top; ++k)
-                if (ids[k] == id[i]) { first = first && k >= j; sum += qs[k]; }
-            if (first) out[id[i]] = from_f32<TS>(g * (dense(at[i]) - sum));
+        if (WAVES > 1) {
+            if (t == 0) shared_Q[sub] = Q;
+            __syncthreads();                           // also: the listed values are read before anything is written
+            Q = shared_Q[sub];
         }
+        const bool none = g == 0.0f || Q == 0.0f, zeros = none || d.normalised || m == PC_NEG_INF_F;
+        const float f = Q * expf(-log_s);
+        auto dense = [&](float v) { return __builtin_amdgcn_exp2f((v - m) * c) * f; };
+        if (listing && !none) {                        // a category listed more than once: its first entry writes for all
+#pragma unroll
+            for (int i = 0; i < G::LIST; ++i) {
+                const int j = t + i * TH;
+                bool first = list.id[i] >= 0;
+                float sum = 0.0f;
+                for (int k = 0; k < d.top; ++k) {
+                    const int32_t o = LONG ? ids[k] : __builtin_amdgcn_readlane(list.id[0], k);
+                    const float oq = LONG ? qs[k] : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.q[0]), k));
+                    if (o == list.id[i]) { first = first && k >= j; sum += oq; }
+                }
+                at[i] = g * ((zeros ? 0.0f : dense(at[i])) - sum);
+                if (!first) list.id[i] = -1;
+            }
+        }
+        const int off = elements_off(out);
+        const TS *zg = z - off;                        // element i of the grid is category i - off
+        TS *grid = out - off;
+        const int64_t end = off + (int64_t)d.n_cats, packs = (end + N - 1) / N;
+        for (int64_t p0 = 0; p0 < packs; p0 += kPacks * TH) {
+            Pack<TS> in[kPacks];
+            if (!zeros)
+#pragma unroll
+                for (int k = 0; k < kPacks; ++k) {
+                    const int64_t i = (p0 + t + k * TH) * N;
+                    if (i >= off && i + N <= end) in[k] = load_pack(zg + i);
+                }
+#pragma unroll
+            for (int k = 0; k < kPacks; ++k) {
+                const int64_t i = (p0 + t + k * TH) * N;
+                if (i >= off && i + N <= end) {
+                    float x[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = zeros ? 0.0f : g * dense(to_f32(in[k].v[e]));
+                    *reinterpret_cast<Pack<TS> *>(__builtin_assume_aligned(grid + i, 16)) = pack_f32<TS>(x);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (i + e >= off && i + e < end) grid[i + e] = from_f32<TS>(zeros ? 0.0f : g * dense(to_f32(zg[i + e])));
+                }
+            }
+        }
+        if (WAVES > 1) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        if (listing && !none)
+#pragma unroll
+            for (int i = 0; i < G::LIST; ++i)
+                if (list.id[i] >= 0) out[list.id[i]] = from_f32<TS>(at[i]);
+        if (WAVES > 1) __syncthreads();                // LDS is read
     }
 }
 
@@ -186,7 +305,19 @@ static DistillDev distill_dev(const pc_distill *d)
     return DistillDev{d->rows, d->student_ld, d->ids_ld, d->teacher_ld, d->n_cats, d->top, d->student, d->teacher, d->ids, d->teacher_lse,
                       1.0f / d->temperature, d->normalised != 0};
 }
-static unsigned row_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 << 20); }
+// f(waves of a row, whether its list is long), as types: one wave where a row is at most 2048 elements, sixteen where there are fewer rows than
+// two a CU, else four.
+template <typename F>
+static void with_group(const pc_distill *d, F f)
+{
+    const bool long_list = d->top > kShortList;
+    if (long_list) f(Group<4, true>{});
+    else if (d->n_cats <= 2048) f(Group<1, false>{});
+    else if (d->rows < 512) f(Group<16, false>{});
+    else f(Group<4, false>{});
+}
+template <typename G>
+static dim3 row_grid(int64_t rows) { return dim3((unsigned)std::min<int64_t>((rows + G::ROWS - 1) / G::ROWS, 1 << 20)); }
 
 // first and last byte of `rows` rows
 static bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
@@ -223,8 +354,11 @@ pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t worksp
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            hipLaunchKernelGGL((k_distill_rows<decltype(s), decltype(t)>), dim3(row_grid(d->rows)), dim3(kRowThreads), 0, (hipStream_t)stream, dev, loss,
-                               stats);
+            with_group(d, [&](auto g) {
+                using G = decltype(g);
+                hipLaunchKernelGGL((k_distill_rows<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
+                                   (hipStream_t)stream, dev, loss, stats);
+            });
         });
     });
     return launched();
@@ -244,8 +378,11 @@ pc_status pc_distill_backward(const pc_distill *d, const float *stats, const flo
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            hipLaunchKernelGGL((k_distill_grad<decltype(s), decltype(t)>), dim3(row_grid(d->rows)), dim3(kRowThreads), 0, (hipStream_t)stream, dev, stats,
-                               dloss, scale, dstudent, dstudent_ld);
+            with_group(d, [&](auto g) {
+                using G = decltype(g);
+                hipLaunchKernelGGL((k_distill_grad<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
+                                   (hipStream_t)stream, dev, stats, dloss, scale, dstudent, dstudent_ld);
+            });
         });
     });
     return launched();

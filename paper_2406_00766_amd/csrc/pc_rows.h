@@ -6,6 +6,7 @@
 
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "pc_internal.h"
 
@@ -29,6 +30,35 @@ template <> __device__ inline bf16_t from_f32<bf16_t>(float v)
     const uint32_t u = __float_as_uint(v);
     return bf16_t{(uint16_t)(v != v ? (u >> 16) | 0x40 : (u + 0x7fff + ((u >> 16) & 1)) >> 16)};
 }
+
+// Eight 16-bit or four 32-bit elements, 16 bytes, at any address that suits an element.
+template <typename T> struct Pack { static constexpr int N = 16 / sizeof(T); T v[N]; };
+template <typename T>
+__device__ inline Pack<T> load_pack(const T *p) { Pack<T> r; __builtin_memcpy(&r, p, 16); return r; }
+template <typename T>
+__device__ inline void store_pack(T *p, const Pack<T> &v) { __builtin_memcpy(p, &v, 16); }
+typedef float pc_float2 __attribute__((ext_vector_type(2)));
+typedef __bf16 pc_bf16x2 __attribute__((ext_vector_type(2)));
+template <typename T>
+__device__ inline Pack<T> pack_f32(const float (&x)[Pack<T>::N])
+{
+    Pack<T> r;
+    if constexpr (sizeof(T) == 2 && !std::is_same<T, f16_t>::value) {
+#pragma unroll
+        for (int i = 0; i < Pack<T>::N; i += 2) {
+            const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector((pc_float2){x[i], x[i + 1]}, pc_bf16x2));
+            r.v[i] = bf16_t{(uint16_t)w};
+            r.v[i + 1] = bf16_t{(uint16_t)(w >> 16)};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < Pack<T>::N; ++i) r.v[i] = from_f32<T>(x[i]);
+    }
+    return r;
+}
+// elements before the first 16-byte boundary at or after p's own 16 bytes begin: p is element `off` of an aligned row
+template <typename T>
+__device__ inline int elements_off(const T *p) { return (int)(((uintptr_t)p & 15) / sizeof(T)); }
 
 inline int64_t type_bytes(int32_t type) { return type == PC_F32 ? 4 : 2; }
 inline bool type_known(int32_t type) { return type == PC_F32 || type == PC_BF16 || type == PC_F16; }
