@@ -367,18 +367,27 @@ def pc_measure_mfma_f32(out_buf, out_bytes: int, reps: int = 5, stream=None) -> 
 
 
 # ---- token models over circuits: these take torch tensors, whose shapes, types and strides become the descriptors ----
+# The kernels trust what is passed on from here, so everything is checked; a tensor that is plainly right passes _fits (calls of a few
+# microseconds are common in decoding), any other goes through _tensor, which accepts strided rows and says what is wrong.
 def _refuse(message: str):
     raise PcError(1, message)
 
 
-def _tensor(name, t, dtype=None, shape=None, device=None, last=1):
-    """Check one argument: a tensor on the GPU (on `device`), of this type and shape (None: any length), its last `last` axes
-    contiguous.  The kernels trust what is passed on from here."""
+def _fits(t, dtype, shape, index) -> bool:
+    """A contiguous tensor on GPU `index` of this type and shape."""
+    try:
+        return t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()
+    except AttributeError:
+        return False
+
+
+def _tensor(name, t, dtype=None, shape=None, index=None, last=1):
+    """Check one argument: a tensor on the GPU (on GPU `index`), of this type and shape (None: any length), its last `last` axes contiguous."""
     import torch
     if not isinstance(t, torch.Tensor):
         _refuse(f"{name} must be a tensor")
-    if t.device.type != "cuda" or (device is not None and t.device != device):
-        _refuse(f"{name} must lie on {device if device is not None else 'a GPU'}, not on {t.device}")
+    if t.device.type != "cuda" or (index is not None and t.get_device() != index):
+        _refuse(f"{name} must lie on {'a GPU' if index is None else f'GPU {index}'}, not on {t.device}")
     if dtype is not None and t.dtype != dtype:
         _refuse(f"{name} must be {dtype}, not {t.dtype}")
     if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
@@ -393,28 +402,40 @@ def _tensor(name, t, dtype=None, shape=None, device=None, last=1):
 
 def _ld(t):
     """Elements between the rows of a matrix (its length where there is but one row, whose stride means nothing)."""
-    n = t.shape[1]
-    if t.shape[0] > 1 and t.stride(0) < n:
+    rows, n = t.shape
+    if rows <= 1:
+        return n
+    ld = t.stride(0)
+    if ld < n:
         _refuse("the rows of a matrix must not overlap")
-    return t.stride(0) if t.shape[0] > 1 else n
+    return ld
+
+
+_types = {}
 
 
 def _type(name, t):
-    import torch
-    types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # PC_F32, PC_BF16, PC_F16
-    if t.dtype not in types:
+    if not _types:
+        import torch
+        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})     # PC_F32, PC_BF16, PC_F16
+    code = _types.get(t.dtype)
+    if code is None:
         _refuse(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
-    return types[t.dtype]
+    return code
 
 
-def _call(device, stream, function, *args):
-    """function(*args, stream) with `device` current; stream None: that device's current stream."""
+def _call(index, stream, function, *args):
+    """function(*args, stream) with GPU `index` current; stream None: that GPU's current stream."""
     import torch
-    if device.index is None or device.index == torch.cuda.current_device():
-        _check(function(*args, _stream(stream)))
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(index)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        _check(function(*args, stream))
     else:
-        with torch.cuda.device(device):
-            _check(function(*args, _stream(stream)))
+        with torch.cuda.device(index):
+            _check(function(*args, stream))
 
 
 class mixture:
@@ -424,10 +445,10 @@ class mixture:
     def __init__(self, weights, K, n_cats, n_blocks, rows=None, table=None, n_tables=None):
         import torch
         _tensor("weights", weights, torch.float32, (None, None))
-        self.device, self.columns = weights.device, int(weights.shape[1])
+        self.index, self.columns = weights.get_device(), int(weights.shape[1])
         for name, t in (("rows", rows), ("table", table)):
             if t is not None:
-                _tensor(name, t, torch.int32, (n_blocks,), self.device)
+                _tensor(name, t, torch.int32, (n_blocks,), self.index)
         self.keep = (weights, rows, table)
         self.struct = pc_mixture(int(K), int(n_blocks), int(n_cats), int(n_blocks if n_tables is None else n_tables), int(weights.shape[0]),
                                  _ld(weights), weights.data_ptr(), _ptr(rows), _ptr(table))
@@ -438,37 +459,47 @@ def pc_get_mixture(handle, var, B, workspace, workspace_bytes) -> mixture:
     m = mixture.__new__(mixture)
     m.struct = pc_mixture()
     _check(lib().pc_get_mixture(handle, int(var), int(B), _ptr(workspace), int(workspace_bytes), C.byref(m.struct)))
-    m.device, m.columns, m.keep = workspace.device, int(m.struct.stride), (workspace,)
+    m.index, m.columns, m.keep = workspace.get_device(), int(m.struct.stride), (workspace,)
     return m
 
 
-def _check_predict(m, tables, B, name, out):
+def _floats(name, t, n, index):
+    """A contiguous float32 tensor of n elements, of any shape."""
     import torch
-    s = m.struct
-    _tensor("tables", tables, torch.float32, None, m.device, tables.dim() if isinstance(tables, torch.Tensor) else 1)
-    if tables.numel() != s.n_tables * s.n_cats * s.K:
-        _refuse(f"tables must hold {s.n_tables} x {s.n_cats} x {s.K} floats")
-    if B > m.columns:
-        _refuse("weights have fewer than B columns")
-    _tensor(name, out, torch.float32, (B, s.n_cats), m.device)
+    _tensor(name, t, torch.float32, None, index, t.dim() if isinstance(t, torch.Tensor) else 1)
+    if t.numel() != n:
+        _refuse(f"{name} must hold {n} floats, not {t.numel()}")
+
+
+def _rows(name, t, dtype, shape, index):
+    if not _fits(t, dtype, shape, index):
+        _tensor(name, t, dtype, shape, index)
+    return t.data_ptr(), _ld(t)
 
 
 def pc_predict(m: mixture, tables, B, logp, stream=None):
     """logp float32 [B, n_cats] (rows may be strided) = log sum of weights * tables."""
-    _check_predict(m, tables, B, "logp", logp)
-    _call(m.device, stream, lib().pc_predict, C.byref(m.struct), tables.data_ptr(), int(B), logp.data_ptr(), _ld(logp))
+    import torch
+    s, B = m.struct, int(B)
+    _floats("tables", tables, s.n_tables * s.n_cats * s.K, m.index)
+    if B > m.columns:
+        _refuse("weights have fewer than B columns")
+    out = _rows("logp", logp, torch.float32, (B, s.n_cats), m.index)
+    _call(m.index, stream, lib().pc_predict, C.byref(s), tables.data_ptr(), B, *out)
 
 
 def pc_predict_backward(m: mixture, tables, B, logp, dlogp, scale, table_flow, accumulate=True, stream=None):
     """Table flows for a gradient dlogp [B, n_cats] of an objective; added to table_flow, or stored."""
     import torch
-    _check_predict(m, tables, B, "logp", logp)
-    _tensor("dlogp", dlogp, torch.float32, (B, m.struct.n_cats), m.device)
-    _tensor("table_flow", table_flow, torch.float32, None, m.device, table_flow.dim() if isinstance(table_flow, torch.Tensor) else 1)
-    if table_flow.numel() != tables.numel():
-        _refuse("table_flow must be as long as tables")
-    _call(m.device, stream, lib().pc_predict_backward, C.byref(m.struct), tables.data_ptr(), int(B), logp.data_ptr(), _ld(logp),
-          dlogp.data_ptr(), _ld(dlogp), float(scale), int(bool(accumulate)), table_flow.data_ptr())
+    s, B = m.struct, int(B)
+    n = s.n_tables * s.n_cats * s.K
+    _floats("tables", tables, n, m.index)
+    _floats("table_flow", table_flow, n, m.index)
+    if B > m.columns:
+        _refuse("weights have fewer than B columns")
+    shape = (B, s.n_cats)
+    _call(m.index, stream, lib().pc_predict_backward, C.byref(s), tables.data_ptr(), B, *_rows("logp", logp, torch.float32, shape, m.index),
+          *_rows("dlogp", dlogp, torch.float32, shape, m.index), float(scale), 1 if accumulate else 0, table_flow.data_ptr())
 
 
 class distill:
@@ -477,17 +508,18 @@ class distill:
     def __init__(self, student, ids, teacher, temperature=1.0, teacher_lse=None, normalised=False):
         import torch
         _tensor("student", student, None, (None, None))
-        self.device = student.device
-        rows = int(student.shape[0])
-        _tensor("ids", ids, torch.int32, (rows, None), self.device)
-        _tensor("teacher", teacher, None, (rows, ids.shape[1]), self.device)
+        self.index = index = student.get_device()
+        self.student, self.keep = student, (ids, teacher, teacher_lse)
+        self.rows, n_cats = student.shape
+        if not (isinstance(ids, torch.Tensor) and ids.dim() == 2 and _fits(ids, torch.int32, (self.rows, ids.shape[1]), index)):
+            _tensor("ids", ids, torch.int32, (self.rows, None), index)
+        if not (isinstance(teacher, torch.Tensor) and _fits(teacher, teacher.dtype, ids.shape, index)):
+            _tensor("teacher", teacher, None, tuple(ids.shape), index)
         if teacher_lse is not None:
-            _tensor("teacher_lse", teacher_lse, torch.float32, (rows,), self.device)
-        self.keep = (student, ids, teacher, teacher_lse)
-        self.student = student
-        self.struct = pc_distill(rows, int(student.shape[1]), int(ids.shape[1]), student.data_ptr(), _type("student", student), _ld(student),
-                                 ids.data_ptr(), _ld(ids), teacher.data_ptr(), _type("teacher", teacher), _ld(teacher),
-                                 _ptr(teacher_lse), float(temperature), int(bool(normalised)))
+            _tensor("teacher_lse", teacher_lse, torch.float32, (self.rows,), index)
+        self.struct = pc_distill(self.rows, n_cats, ids.shape[1], student.data_ptr(), _type("student", student), _ld(student), ids.data_ptr(),
+                                 _ld(ids), teacher.data_ptr(), _type("teacher", teacher), _ld(teacher), _ptr(teacher_lse),
+                                 temperature, 1 if normalised else 0)
 
 
 def pc_distill_workspace_bytes(d: distill) -> int:
@@ -496,30 +528,34 @@ def pc_distill_workspace_bytes(d: distill) -> int:
     return int(n.value)
 
 
-def _workspace(t, device):
+def _workspace(t, index):
     import torch
     if t is None:
         return None, 0
-    _tensor("workspace", t, torch.uint8, (None,), device)
+    if not (isinstance(t, torch.Tensor) and _fits(t, torch.uint8, (t.numel(),), index)):
+        _tensor("workspace", t, torch.uint8, (None,), index)
     return t.data_ptr(), t.numel()
+
+
+def _array(name, t, dtype, shape, index):
+    if not _fits(t, dtype, shape, index):
+        _tensor(name, t, dtype, shape, index, len(shape))
+    return t.data_ptr()
 
 
 def pc_distill_forward(d: distill, workspace, loss, stats, stream=None):
     """loss float32 [rows], stats float32 [rows, 2]."""
     import torch
-    _tensor("loss", loss, torch.float32, (d.struct.rows,), d.device)
-    _tensor("stats", stats, torch.float32, (d.struct.rows, 2), d.device, 2)
-    _call(d.device, stream, lib().pc_distill_forward, C.byref(d.struct), *_workspace(workspace, d.device), loss.data_ptr(), stats.data_ptr())
+    _call(d.index, stream, lib().pc_distill_forward, C.byref(d.struct), *_workspace(workspace, d.index),
+          _array("loss", loss, torch.float32, (d.rows,), d.index), _array("stats", stats, torch.float32, (d.rows, 2), d.index))
 
 
 def pc_distill_backward(d: distill, stats, dloss, scale, dstudent, stream=None):
     """dstudent [rows, n_cats] of the student's type = scale * dloss (float32 [rows] or None) * gradient; it may be the student itself."""
     import torch
-    _tensor("stats", stats, torch.float32, (d.struct.rows, 2), d.device, 2)
-    if dloss is not None:
-        _tensor("dloss", dloss, torch.float32, (d.struct.rows,), d.device)
-    _tensor("dstudent", dstudent, d.student.dtype, tuple(d.student.shape), d.device)
-    _call(d.device, stream, lib().pc_distill_backward, C.byref(d.struct), stats.data_ptr(), _ptr(dloss), float(scale), dstudent.data_ptr(), _ld(dstudent))
+    _call(d.index, stream, lib().pc_distill_backward, C.byref(d.struct), _array("stats", stats, torch.float32, (d.rows, 2), d.index),
+          None if dloss is None else _array("dloss", dloss, torch.float32, (d.rows,), d.index), float(scale),
+          *_rows("dstudent", dstudent, d.student.dtype, d.student.shape, d.index))
 
 
 class beam:
@@ -528,16 +564,19 @@ class beam:
     def __init__(self, scores, running, n_out, done=None, done_token=0, normalise=False):
         import torch
         _tensor("scores", scores, None, (None, None))
-        self.device = scores.device
-        _tensor("running", running, torch.float32, (None, None), self.device, 2)
-        groups, beams = int(running.shape[0]), int(running.shape[1])
-        if scores.shape[0] != groups * beams:
+        self.index = index = scores.get_device()
+        if not (isinstance(running, torch.Tensor) and running.dim() == 2 and _fits(running, torch.float32, running.shape, index)):
+            _tensor("running", running, torch.float32, (None, None), index, 2)
+        groups, beams = running.shape
+        rows, n_cats = scores.shape
+        if rows != groups * beams:
             _refuse("scores must have a row for each running score")
         if done is not None:
-            _tensor("done", done, torch.uint8, (groups, beams), self.device, 2)
+            _array("done", done, torch.uint8, (groups, beams), index)
         self.keep = (scores, running, done)
-        self.struct = pc_beam(groups, beams, int(scores.shape[1]), int(n_out), scores.data_ptr(), _type("scores", scores), _ld(scores),
-                              int(bool(normalise)), running.data_ptr(), _ptr(done), int(done_token))
+        self.shape = (groups, int(n_out))
+        self.struct = pc_beam(groups, beams, n_cats, self.shape[1], scores.data_ptr(), _type("scores", scores), _ld(scores),
+                              1 if normalise else 0, running.data_ptr(), _ptr(done), int(done_token))
 
 
 def pc_beam_workspace_bytes(a: beam) -> int:
@@ -549,11 +588,9 @@ def pc_beam_workspace_bytes(a: beam) -> int:
 def pc_beam_select(a: beam, workspace, out_scores, parents, tokens, stream=None):
     """The n_out best of each group: out_scores float32, parents int32 and tokens int32, all [groups, n_out]."""
     import torch
-    shape = (a.struct.groups, a.struct.n_out)
-    for name, t, dtype in (("out_scores", out_scores, torch.float32), ("parents", parents, torch.int32), ("tokens", tokens, torch.int32)):
-        _tensor(name, t, dtype, shape, a.device, 2)
-    _call(a.device, stream, lib().pc_beam_select, C.byref(a.struct), *_workspace(workspace, a.device), out_scores.data_ptr(),
-          parents.data_ptr(), tokens.data_ptr())
+    shape, index = a.shape, a.index
+    _call(index, stream, lib().pc_beam_select, C.byref(a.struct), *_workspace(workspace, index), _array("out_scores", out_scores, torch.float32, shape, index),
+          _array("parents", parents, torch.int32, shape, index), _array("tokens", tokens, torch.int32, shape, index))
 
 
 def pc_beam_reorder(states, parents, beams, stream=None):
@@ -561,23 +598,26 @@ def pc_beam_reorder(states, parents, beams, stream=None):
     a row's elements are contiguous, rows may be strided."""
     import torch
     _tensor("parents", parents, torch.int32, (None, None), None, 2)
-    groups, n_out, beams = int(parents.shape[0]), int(parents.shape[1]), int(beams)
+    groups, n_out = parents.shape
+    beams, index = int(beams), parents.get_device()
     if not 1 <= len(states) <= 16:
         _refuse("1 .. 16 states")
     array = (pc_state * len(states))()
     for s, (src, dst) in zip(array, states):
         for name, t, rows in (("src", src, groups * beams), ("dst", dst, groups * n_out)):
-            _tensor(name, t, None, None, parents.device, max(1, t.dim() - 1) if isinstance(t, torch.Tensor) else 1)
+            if not (isinstance(t, torch.Tensor) and t.get_device() == index and t.is_contiguous()):
+                _tensor(name, t, None, None, index, max(1, t.dim() - 1) if isinstance(t, torch.Tensor) else 1)
             if t.dim() < 1 or t.shape[0] != rows:
                 _refuse(f"{name} must have {rows} rows")
-        if src.dtype != dst.dtype or src.shape[1:] != dst.shape[1:]:
+        shape = src.shape[1:]
+        if src.dtype != dst.dtype or shape != dst.shape[1:]:
             _refuse("src and dst must have rows of one shape and type")
-        n = src[:1].numel() if src.shape[0] else 1
         e = src.element_size()
-        s.src, s.dst, s.row_bytes = src.data_ptr(), dst.data_ptr(), n * e
-        s.src_stride = src.stride(0) * e if src.shape[0] > 1 else n * e
-        s.dst_stride = dst.stride(0) * e if dst.shape[0] > 1 else n * e
-    _call(parents.device, stream, lib().pc_beam_reorder, array, len(states), parents.data_ptr(), groups, beams, n_out)
+        n = shape.numel() * e
+        s.src, s.dst, s.row_bytes = src.data_ptr(), dst.data_ptr(), n
+        s.src_stride = src.stride(0) * e if src.shape[0] > 1 else n
+        s.dst_stride = dst.stride(0) * e if dst.shape[0] > 1 else n
+    _call(index, stream, lib().pc_beam_reorder, array, len(states), parents.data_ptr(), groups, beams, n_out)
 
 
 def compiled_tables(handle: int) -> list[dict]:

@@ -44,47 +44,90 @@ __device__ inline float running_score(const BeamDev &a, int64_t row)
 }
 
 // ---- sorting across the lanes of a wave, best first ----
-// Candidates of different beams: score, then lower `place` (beam, then rank within the beam).
+// Candidates of different beams: score, then lower beam, then the key of its row.
 struct Cand {
     double score;
-    uint32_t place;
-    int32_t token;
+    uint64_t key;
+    int32_t beam;
 };
-constexpr uint32_t kNoPlace = ~0u;
-__device__ inline float lane_xor(float v, int j) { return __shfl_xor(v, j); }
-__device__ inline uint64_t lane_xor(uint64_t v, int j) { return __shfl_xor((unsigned long long)v, j); }
-__device__ inline Cand lane_xor(const Cand &v, int j) { return Cand{__shfl_xor(v.score, j), (uint32_t)__shfl_xor((int)v.place, j), __shfl_xor(v.token, j)}; }
+// the value of lane ^ J: within 16 lanes by data-parallel moves, across them by swaps of rows and halves
+template <int J>
+__device__ inline uint32_t lane_xor32(uint32_t v)
+{
+    const int x = (int)v;
+    if constexpr (J == 1) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0xb1, 0xf, 0xf, false);            // quad_perm 1 0 3 2
+    else if constexpr (J == 2) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x4e, 0xf, 0xf, false);       // quad_perm 2 3 0 1
+    else if constexpr (J == 4) {                       // four lanes up for the even fours of a row, four down for the odd ones
+        const int up = __builtin_amdgcn_update_dpp(x, x, 0x104, 0xf, 0x5, false);
+        return (uint32_t)__builtin_amdgcn_update_dpp(up, x, 0x114, 0xf, 0xa, false);
+    } else if constexpr (J == 8) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, false);    // row_ror 8
+    else if constexpr (J == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+}
+template <int J> __device__ inline float lane_xor(float v) { return __uint_as_float(lane_xor32<J>(__float_as_uint(v))); }
+template <int J> __device__ inline uint64_t lane_xor(uint64_t v) { return (uint64_t)lane_xor32<J>((uint32_t)(v >> 32)) << 32 | lane_xor32<J>((uint32_t)v); }
 __device__ inline bool better(float a, float b) { return a > b; }
 __device__ inline bool better(uint64_t a, uint64_t b) { return a > b; }
-__device__ inline bool better(const Cand &a, const Cand &b) { return a.score > b.score || (a.score == b.score && a.place < b.place); }
-// One step: of a lane and its partner j away the better stays in the one chosen by `first`.
-template <typename V>
-__device__ inline V exchange(const V &v, int j, bool first)
+__device__ inline bool better(const Cand &a, const Cand &b) { return a.score > b.score || (a.score == b.score && (a.beam < b.beam || (a.beam == b.beam && a.key > b.key))); }
+// Exchanges over J, J / 2 .. 1 lanes: of a lane and its partner the one whose bit J is clear keeps the better where `up`, the worse elsewhere.
+// Keys are distinct, or equal in all that counts.
+template <int J, typename V>
+__device__ inline V exchanges(const V &v, bool up)
 {
-    const V o = lane_xor(v, j);
-    return better(o, v) == first ? o : v;              // keys are distinct, or equal in all that counts
+    const V o = lane_xor<J>(v);
+    const V r = better(o, v) == (((threadIdx.x & J) == 0) == up) ? o : v;
+    if constexpr (J > 1) return exchanges<J / 2>(r, up);
+    else return r;
 }
-template <typename V>
-__device__ inline V sort_lanes(V v)
+template <int K = 2, typename V>
+__device__ inline V sort_lanes(const V &v)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-        for (int j = k >> 1; j > 0; j >>= 1) v = exchange(v, j, ((lane & j) == 0) == ((lane & k) == 0));
-    return v;
+    const V r = exchanges<K / 2>(v, K == 64 || (threadIdx.x & K) == 0);
+    if constexpr (K < 64) return sort_lanes<K * 2>(r);
+    else return r;
 }
 // The 64 best of two sorted lists; `other` holds the second one in reverse (lane i: its entry 63 - i).
 template <typename V>
 __device__ inline V merge_lanes(const V &v, const V &other)
 {
+    const V r = better(other, v) ? other : v;
+    return exchanges<32>(r, true);
+}
+// The same for candidates, in loops: a group's join runs each step once or twice, and code that long would mostly wait for itself to be fetched.
+__device__ inline Cand lane_of(const Cand &v, int lane)
+{
+    return Cand{__shfl(v.score, lane), (uint64_t)__shfl((unsigned long long)v.key, lane), __shfl(v.beam, lane)};
+}
+__device__ inline Cand exchange_step(const Cand &v, int j, bool up)
+{
     const int lane = threadIdx.x & 63;
-    V r = better(other, v) ? other : v;
-#pragma unroll
-    for (int j = 32; j > 0; j >>= 1) r = exchange(r, j, (lane & j) == 0);
+    const Cand o = lane_of(v, lane ^ j);
+    return better(o, v) == (((lane & j) == 0) == up) ? o : v;
+}
+__device__ inline Cand sort_candidates(Cand v)
+{
+#pragma unroll 1
+    for (int kj = 0; kj < 21; ++kj) {                  // (k, j) = (2, 1), (4, 2), (4, 1), (8, 4) .. (64, 1)
+        const int stage = kj < 1 ? 0 : kj < 3 ? 1 : kj < 6 ? 2 : kj < 10 ? 3 : kj < 15 ? 4 : 5, at = kj - stage * (stage + 1) / 2;
+        const int k = 2 << stage;
+        v = exchange_step(v, k >> (at + 1), k == 64 || (threadIdx.x & k) == 0);
+    }
+    return v;
+}
+__device__ inline Cand merge_candidates(const Cand &v, const Cand &other)
+{
+    Cand r = better(other, v) ? other : v;
+#pragma unroll 1
+    for (int j = 32; j > 0; j >>= 1) r = exchange_step(r, j, true);
     return r;
 }
-// n-th largest (n <= 64) of one value per thread.  No NaN.
+// n-th largest (n <= 64) of one value per lane of a wave, or per thread of the workgroup.  No NaN.
+__device__ inline float wave_nth(float v, int n) { return __shfl(sort_lanes(v), n - 1); }
 __device__ inline float block_nth(float v, int n, float (&lds)[kBeamThreads])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -96,295 +139,353 @@ __device__ inline float block_nth(float v, int n, float (&lds)[kBeamThreads])
     for (int w = 1; w < kBeamThreads / 64; ++w) v = merge_lanes(v, lds[(wave + w) % (kBeamThreads / 64) * 64 + 63 - lane]);
     return __shfl(v, n - 1);
 }
-
-// ---- stage 1: the n best of a segment of a row, and its part of the log-normaliser ----
-// A segment passes through registers once, kChunk categories at a time.  The n-th largest of the first chunk's 256 thread maxima is a
-// bound that at least n categories reach; what reaches it (some 1.1 n of a chunk) goes to a list in LDS, and later chunks add
-// what lies above it, for a category further back loses a tie.  Should the list overflow (rows in ascending order, ties), the bound is
-// raised by the chunk's own maxima, then by the list cut to its n best, and as a last resort the chunk goes through the list 256 at a time.
-constexpr int kElems = 16, kChunk = kBeamThreads * kElems, kList = 1024;
-struct RowPart { float m; float pad; double sum; };    // maximum and sum of exp(z - m) of a segment
-
-template <typename T> struct Vec { static constexpr int N = 16 / sizeof(T); };
-
-// The categories of a chunk: virtual index i (category + off, where off is the row's distance from a 16-byte boundary) of element e.
-template <typename T>
-__device__ inline int64_t elem_index(int64_t base, int e)
-{
-    constexpr int N = Vec<T>::N;
-    return base + (e / N) * (kBeamThreads * N) + threadIdx.x * N + e % N;
-}
-// -inf outside [lo, hi)
-template <typename T>
-__device__ inline void load_chunk(const T *row, int64_t base, int64_t lo, int64_t hi, float (&v)[kElems])
-{
-    constexpr int N = Vec<T>::N;
-#pragma unroll
-    for (int j = 0; j < kElems / N; ++j) {
-        const int64_t i = elem_index<T>(base, j * N);
-        if (i >= lo && i + N <= hi) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(row + i);
-            const T *t = reinterpret_cast<const T *>(&q);
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[j * N + k] = to_f32(t[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[j * N + k] = i + k >= lo && i + k < hi ? to_f32(row[i + k]) : PC_NEG_INF_F;
-        }
-    }
-}
-
-struct BeamLds {
-    uint64_t list[kList], kept[64];
-    float nth[kBeamThreads];
-    int count;
-};
-
-// Cut the list to its n best, in order; returns the n-th (0: fewer).  All threads; the list is complete and synchronised.
-__device__ inline uint64_t cut_list(BeamLds &s, int n)
-{
-    int count = s.count;
-    if (count > 128) {                                 // a bound from thread maxima leaves few for the ranking
-        float mine = PC_NEG_INF_F;
-        for (int i = threadIdx.x; i < count; i += kBeamThreads) mine = fmaxf(mine, key_value((uint32_t)(s.list[i] >> 32)));
-        const uint32_t bound = order_key(block_nth(mine, n, s.nth));
-        uint64_t held[kList / kBeamThreads];
-#pragma unroll
-        for (int i = 0; i < kList / kBeamThreads; ++i) held[i] = threadIdx.x + i * kBeamThreads < count ? s.list[threadIdx.x + i * kBeamThreads] : 0;
-        __syncthreads();
-        if (threadIdx.x == 0) s.count = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kList / kBeamThreads; ++i)
-            if (held[i] && (uint32_t)(held[i] >> 32) >= bound) s.list[atomicAdd(&s.count, 1)] = held[i];
-        __syncthreads();
-        count = s.count;
-    }
-    if (threadIdx.x < 64) s.kept[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < count; i += kBeamThreads) {
-        const uint64_t k = s.list[i];
-        int rank = 0;
-        for (int j = 0; j < count; ++j) rank += s.list[j] > k;
-        if (rank < n) s.kept[rank] = k;
-    }
-    __syncthreads();
-    if (threadIdx.x < n) s.list[threadIdx.x] = s.kept[threadIdx.x];
-    if (threadIdx.x == 0) s.count = min(count, n);
-    __syncthreads();
-    return s.kept[n - 1];
-}
-
 // the next float up; above +inf: NaN, which nothing reaches
 __device__ inline float next_above(float t) { return key_value(order_key(t) + 1); }
+
+// ---- stage 1: the n best of a segment of a row, and its part of the log-normaliser ----
+// A segment passes through registers once, four 16-byte packs a lane at a time, the next ones on their way.  The n-th largest of the first
+// chunk's 256 thread maxima is a bound that at least n categories reach; what reaches it (some 1.1 n of a chunk) goes to the wave's list
+// in LDS, and later chunks add what lies above it, for a category further back loses a tie.  Should a list overflow (rows in
+// ascending order, ties), the wave raises its bound by the chunk's own maxima, then by its list cut to the n best, and as a last resort
+// passes the chunk through the list an element a lane at a time.  Waves do not wait for each other between the first bound and the end.  Bound
+// by instructions: maximum, exponential, comparison per element (256 x 16 x 50257 bf16, a quarter of the beams at rest: see the table of cases).
+constexpr int kBeamPacks = 4, kWaveList = 256, kBeamWaves = kBeamThreads / 64;
+template <typename T> constexpr int chunk_elements() { return kBeamThreads * kBeamPacks * Pack<T>::N; }
+struct RowPart { float m; float pad; double sum; };    // maximum and sum of exp(z - m) of a segment
+
+// A wave's list and its length.
+struct WaveList {
+    uint64_t *list;
+    int count;
+    // the 64 best in order, a lane each; the list becomes the first n of them
+    __device__ inline uint64_t cut(int n)
+    {
+        const int lane = threadIdx.x & 63;
+        uint64_t v = sort_lanes(lane < count ? list[lane] : 0), nth = __shfl((unsigned long long)v, n - 1);
+        for (int i = 64; i < count; i += 64) {
+            uint64_t w = i + lane < count ? list[i + lane] : 0;
+            if (!__any(w > nth)) continue;
+            w = sort_lanes(w);
+            v = merge_lanes(v, (uint64_t)__shfl((unsigned long long)w, 63 - lane));
+            nth = __shfl((unsigned long long)v, n - 1);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        count = min(count, n);
+        if (lane < count) list[lane] = v;
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        return v;
+    }
+    __device__ inline void add(uint64_t key, bool on)   // room for 64
+    {
+        const uint64_t those = __ballot(on);
+        if (on) list[count + __popcll(those & ((1ull << (threadIdx.x & 63)) - 1))] = key;
+        count += __popcll(those);
+    }
+};
 
 template <typename T>
 __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int32_t n_seg, int32_t seg_len, uint64_t *__restrict__ best,
                                                             RowPart *__restrict__ parts)
 {
-    __shared__ BeamLds s;
-    __shared__ float wave_m[kBeamThreads / 64];
-    __shared__ double wave_sum[kBeamThreads / 64];
+    constexpr int N = Pack<T>::N, ELEMS = kBeamPacks * N, CHUNK = chunk_elements<T>();
+    __shared__ uint64_t lists[kBeamWaves][kWaveList];
+    __shared__ float nth_lds[kBeamThreads], wave_m[kBeamWaves];
+    __shared__ double wave_sum[kBeamWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n_out;
     const int64_t tasks = (int64_t)a.groups * a.beams * n_seg;
     for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
         const int64_t r = task / n_seg;
         if ((a.done && a.done[r]) || running_score(a, r) == PC_NEG_INF_F) continue;       // the join knows these beams' candidates
+        // category c is element c + off of a grid of 16-byte packs; none before off is read
         const T *z = (const T *)a.scores + r * a.ld;
-        const int64_t off = ((uintptr_t)z & 15) / sizeof(T);
-        const T *row = z - off;                        // category c is element c + off; none before off is read
-        const int64_t first = (task % n_seg) * (int64_t)seg_len, hi = min(off + a.n_cats, first + seg_len), lo = max(off, first);
+        const int off = elements_off(z);
+        const T *grid = z - off;
+        const int64_t first = (task % n_seg) * (int64_t)seg_len, hi = min((int64_t)off + a.n_cats, first + seg_len), lo = max((int64_t)off, first);
         float m = PC_NEG_INF_F, sum = 0.0f, t = PC_NEG_INF_F;
-        __syncthreads();
-        if (threadIdx.x == 0) s.count = 0;
-        __syncthreads();
-        float v[kElems], ahead[kElems];
-        load_chunk(row, first, lo, hi, ahead);
-        for (int64_t base = first; base < hi; base += kChunk) {
+        WaveList mine{lists[wave], 0};
+        Pack<T> ahead[kBeamPacks];
+        auto index = [&](int64_t base, int k) { return base + ((int64_t)k * kBeamThreads + threadIdx.x) * N; };
+        auto fetch = [&](int64_t base) {               // whole packs
 #pragma unroll
-            for (int e = 0; e < kElems; ++e) v[e] = ahead[e];
-            if (base + kChunk < hi) load_chunk(row, base + kChunk, lo, hi, ahead);
+            for (int k = 0; k < kBeamPacks; ++k)
+                if (index(base, k) >= lo && index(base, k) + N <= hi) ahead[k] = *reinterpret_cast<const Pack<T> *>(__builtin_assume_aligned(grid + index(base, k), 16));
+        };
+        fetch(first);
+        for (int64_t base = first; base < hi; base += CHUNK) {
+            const bool inner = base >= lo && base + CHUNK <= hi;
+            float v[ELEMS];                            // -inf outside [lo, hi)
+#pragma unroll
+            for (int k = 0; k < kBeamPacks; ++k) {
+                const int64_t i = index(base, k);
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[k * N + e] = to_f32(ahead[k].v[e]);
+                if (!inner && !(i >= lo && i + N <= hi))
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[k * N + e] = i + e >= lo && i + e < hi ? to_f32(grid[i + e]) : PC_NEG_INF_F;
+            }
+            if (base + CHUNK < hi) fetch(base + CHUNK);
             float top = v[0];
 #pragma unroll
-            for (int e = 1; e < kElems; ++e) top = fmaxf(top, v[e]);
+            for (int e = 1; e < ELEMS; ++e) top = fmaxf(top, v[e]);
             top = fmaxf(top, PC_NEG_INF_F);            // NaN alone
             if (a.normalise) {
                 if (top > m) { sum *= exp2f((m - top) * PC_LOG2E_F); m = top; }
                 const float at = m == PC_NEG_INF_F ? 0.0f : m;
                 float part = 0.0f;
 #pragma unroll
-                for (int e = 0; e < kElems; ++e) part += __builtin_amdgcn_exp2f((v[e] - at) * PC_LOG2E_F);
+                for (int e = 0; e < ELEMS; ++e) part += __builtin_amdgcn_exp2f((v[e] - at) * PC_LOG2E_F);
                 sum += part;
             }
-            bool fresh = false, slow = false;          // fresh: t is reached by n categories of this chunk or before
-            if (t == PC_NEG_INF_F) {
-                t = block_nth(top, n, s.nth);
-                fresh = t > PC_NEG_INF_F;
-                slow = !fresh;
-            }
-            // count what reaches t; room for all of it, or a higher t
-            int mine = 0, at = 0;
+            bool fresh = false;                        // t is reached by n categories of this chunk or before, not above all of them
+            if (base == first) t = block_nth(top, n, nth_lds), fresh = true;
+            else if (t == PC_NEG_INF_F) t = wave_nth(top, n), fresh = true;
+            bool slow = t == PC_NEG_INF_F;
+            int passing = 0;
             for (int attempt = 0; !slow; ++attempt) {
-                mine = 0;
+                passing = 0;
+                if (__any(top >= t))
 #pragma unroll
-                for (int e = 0; e < kElems; ++e) mine += __popcll(__ballot(v[e] >= t));
-                __syncthreads();
-                if (lane == 0 && mine) at = atomicAdd(&s.count, mine);
-                __syncthreads();
-                const int total = s.count;
-                if (total <= kList) break;
-                __syncthreads();
-                if (lane == 0 && mine) atomicSub(&s.count, mine);
-                __syncthreads();
+                    for (int e = 0; e < ELEMS; ++e) passing += __popcll(__ballot(v[e] >= t));
+                if (mine.count + passing <= kWaveList) break;
                 if (attempt == 0) {
-                    const float bound = block_nth(top, n, s.nth);
+                    const float bound = wave_nth(top, n);
                     if (!(bound < t)) { t = bound; fresh = true; }
                 } else if (attempt == 1) {
-                    const uint64_t nth = cut_list(s, n);
+                    const uint64_t v64 = mine.cut(n), nth = __shfl((unsigned long long)v64, n - 1);
                     const float bound = nth ? next_above(key_value((uint32_t)(nth >> 32))) : t;
                     if (bound > t || bound != bound) { t = bound; fresh = false; }
                 } else {
                     slow = true;
                 }
             }
+            auto category = [&](int e) { return (int)(index(base, e / N) + e % N - off); };
             if (!slow) {
-                at = __shfl(at, 0);
-                if (mine)
+                if (passing)
 #pragma unroll
-                    for (int e = 0; e < kElems; ++e) {
-                        const uint64_t on = __ballot(v[e] >= t);
-                        if (on == 0) continue;
-                        if (v[e] >= t) s.list[at + __popcll(on & ((1ull << lane) - 1))] = candidate(v[e], (int)(elem_index<T>(base, e) - off));
-                        at += __popcll(on);
-                    }
+                    for (int e = 0; e < ELEMS; ++e)
+                        if (__any(v[e] >= t)) mine.add(candidate(v[e], category(e)), v[e] >= t);
                 if (fresh) t = next_above(t);
             } else {
                 uint64_t above = 0;                    // only keys above this one count
-                for (int e = 0; e < kElems; ++e) {
-                    __syncthreads();
-                    const bool full = s.count > kList - kBeamThreads;
-                    __syncthreads();                   // all have read it before any adds
-                    if (full) above = cut_list(s, n);
+#pragma unroll 1
+                for (int e = 0; e < ELEMS; ++e) {
+                    if (mine.count > kWaveList - 64) above = __shfl((unsigned long long)mine.cut(n), n - 1);
                     float x = v[0];
 #pragma unroll
-                    for (int f = 1; f < kElems; ++f) x = f == e ? v[f] : x;
-                    const int64_t i = elem_index<T>(base, e);
-                    const uint64_t k = i >= lo && i < hi ? candidate(x, (int)(i - off)) : 0;
-                    if (k > above) s.list[atomicAdd(&s.count, 1)] = k;
+                    for (int f = 1; f < ELEMS; ++f) x = f == e ? v[f] : x;
+                    const int64_t i = index(base, e / N) + e % N;
+                    const uint64_t key = i >= lo && i < hi ? candidate(x, (int)(i - off)) : 0;
+                    mine.add(key, key > above);
                 }
-                __syncthreads();
-                const uint64_t nth = cut_list(s, n);
+                const uint64_t nth = __shfl((unsigned long long)mine.cut(n), n - 1);
                 t = nth ? next_above(key_value((uint32_t)(nth >> 32))) : PC_NEG_INF_F;
             }
         }
+        uint64_t v = mine.cut(n);
+        if (wave > 0) lists[wave][lane] = v;
+        float all = m;
+        for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d));
+        if (lane == 0) wave_m[wave] = all;
         __syncthreads();
-        cut_list(s, n);
-        if (threadIdx.x < n) best[task * n + threadIdx.x] = s.kept[threadIdx.x];
+        if (wave == 0) {
+#pragma unroll
+            for (int w = 1; w < kBeamWaves; ++w) v = merge_lanes(v, lists[w][63 - lane]);
+            if (lane < n) best[task * n + lane] = v;
+        }
         if (a.normalise) {
-            float all = m;
-            for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d));
-            if (lane == 0) wave_m[wave] = all;
-            __syncthreads();
-            for (int w = 0; w < kBeamThreads / 64; ++w) all = fmaxf(all, wave_m[w]);
+            for (int w = 0; w < kBeamWaves; ++w) all = fmaxf(all, wave_m[w]);
             double total = (double)sum * (m == PC_NEG_INF_F ? 1.0 : (double)exp2f((m - all) * PC_LOG2E_F));
             for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
             if (lane == 0) wave_sum[wave] = total;
             __syncthreads();
             if (threadIdx.x == 0) {
                 total = 0.0;
-                for (int w = 0; w < kBeamThreads / 64; ++w) total += wave_sum[w];
+                for (int w = 0; w < kBeamWaves; ++w) total += wave_sum[w];
                 parts[task] = RowPart{all, 0.0f, total};
             }
         }
+        __syncthreads();                               // LDS is read
     }
 }
 
 // ---- stage 2: a group's survivors from its rows' lists ----
-// A wave a beam (up to 16 waves, each taking several beams in turn): the segments' parts of the log-normaliser in 64 bits, the segments'
-// lists merged by key, then by score with the wave's beams before; last the waves' lists, half of them at a time.
-constexpr int kJoinWaves = 16;
+// One workgroup a group.  The log-normalisers of its beams first, in 64 bits; then all entries of all lists, the first of every list before the
+// second of any.  Bound by its chain of loads and comparisons (it moves a few KB): sorting the entries 64 at a time took 10 to 16 us.
+constexpr int kJoinWaves = 16, kRanked = 256;
 __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(const BeamDev a, int32_t n_seg, const uint64_t *__restrict__ best,
                                                                const RowPart *__restrict__ parts, float *__restrict__ out_scores,
                                                                int32_t *__restrict__ parents, int32_t *__restrict__ tokens)
 {
-    __shared__ Cand lists[kJoinWaves][64];
+    __shared__ Cand lists[kJoinWaves][64];             // or the candidates that are ranked
+    __shared__ double norms[PC_MAX_BEAMS], runs[PC_MAX_BEAMS];          // a running score of -inf: nothing but candidates of -inf
+    __shared__ int32_t ended[PC_MAX_BEAMS], rank_of[kRanked], few;
+    __shared__ float least, heads[kJoinWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, n = a.n_out;
-    const Cand none{kNegInf64, kNoPlace, 0};
+    const Cand none{kNegInf64, 0, PC_MAX_BEAMS};       // behind every candidate
     for (int64_t g = blockIdx.x; g < a.groups; g += gridDim.x) {
-        Cand mine = none;
+        const int64_t row0 = g * a.beams;
+        const int n_lists = a.beams * n_seg, n_entries = n_lists * n;
+        // entry e: rank e / n_lists of list e % n_lists (row and segment); read while the normalisers are made
+        const int e0 = threadIdx.x;
+        const uint64_t first = e0 < n_entries ? best[(row0 * n_seg + e0 % n_lists) * n + e0 / n_lists] : 0;
         for (int b = wave; b < a.beams; b += waves) {
-            const int64_t r = g * a.beams + b;
-            const double run = (double)running_score(a, r);
-            const bool done = a.done && a.done[r];
-            bool dead = run == kNegInf64;
+            // everything is requested at once; the part of a beam that is dead or has ended was never written, and is not used
+            const RowPart *p = parts + (row0 + b) * n_seg;
+            const RowPart part = p[min(lane, n_seg - 1)];
+            double run = (double)running_score(a, row0 + b), norm = 0.0;
+            const bool done = a.done && a.done[row0 + b];
+            if (a.normalise && !done && run != kNegInf64) {
+                float m = lane < n_seg ? part.m : PC_NEG_INF_F;
+                for (int i = lane + 64; i < n_seg; i += 64) m = fmaxf(m, p[i].m);
+                for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+                auto term = [&](const RowPart &q) { return q.m == PC_NEG_INF_F ? q.sum : q.sum * exp((double)q.m - (double)m); };
+                double sum = lane < n_seg ? term(part) : 0.0;
+                for (int i = lane + 64; i < n_seg; i += 64) sum += term(p[i]);
+                for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+                norm = (double)m + log(sum);
+                if (!(fabs(norm) < 1e300)) run = kNegInf64;             // no finite number: m is a float
+            }
+            if (lane == 0) {
+                norms[b] = norm;
+                runs[b] = run;
+                ended[b] = done && run != kNegInf64;
+            }
+        }
+        __syncthreads();
+        auto entry = [&](int e) {
             Cand c = none;
-            if (!dead && !done) {
-                double norm = 0.0;
-                if (a.normalise) {
-                    float m = PC_NEG_INF_F;
-                    double sum = 0.0;
-                    for (int i = lane; i < n_seg; i += 64) m = fmaxf(m, parts[r * n_seg + i].m);
-                    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-                    for (int i = lane; i < n_seg; i += 64) {
-                        const RowPart p = parts[r * n_seg + i];
-                        sum += p.m == PC_NEG_INF_F ? p.sum : p.sum * exp((double)p.m - (double)m);
-                    }
-                    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-                    norm = (double)m + log(sum);
-                }
-                dead = !(fabs(norm) < 1e300);          // no finite number: m is a float
-                uint64_t key = 0;
-                for (int s0 = 0; s0 < n_seg; s0 += 8) {
-                    uint64_t next[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        next[i] = s0 + i < n_seg && (s0 + i == 0 ? lane : 63 - lane) < n ? best[(r * n_seg + s0 + i) * n + (s0 + i == 0 ? lane : 63 - lane)] : 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (s0 + i == 0) key = next[i];
-                        else if (s0 + i < n_seg) key = merge_lanes(key, next[i]);
-                }
-                if (key && lane < n) c = Cand{run + ((double)key_value((uint32_t)(key >> 32)) - norm), (uint32_t)(b << 8 | lane), (int32_t)~(uint32_t)key};
+            if (e >= n_entries) return c;
+            const int list = e % n_lists, rank = e / n_lists, b = list / n_seg, seg = list % n_seg;
+            const double run = runs[b];
+            if (run == kNegInf64 || ended[b]) {        // candidates of -inf in order, after the one of a finished beam: from the first segment
+                const int token = !ended[b] ? rank : rank == 0 ? a.done_token : rank <= a.done_token ? rank - 1 : rank;
+                const bool one = ended[b] && rank == 0;
+                if (seg == 0 && rank < a.n_cats) c = Cand{one ? run : kNegInf64, candidate(one ? 0.0f : PC_NEG_INF_F, token), b};
+            } else {
+                const uint64_t key = e == e0 ? first : best[(row0 * n_seg + list) * n + rank];
+                if (key) c = Cand{run + ((double)key_value((uint32_t)(key >> 32)) - norms[b]), key, b};
             }
-            if (dead || done) {                        // candidates of -inf in order, after the one of a finished beam
-                const bool ended = done && !dead;
-                const int token = !ended ? lane : lane == 0 ? a.done_token : lane <= a.done_token ? lane - 1 : lane;
-                c = lane < min(n, a.n_cats) ? Cand{ended && lane == 0 ? run : kNegInf64, (uint32_t)(b << 8 | lane), token} : none;
+            return c;
+        };
+        // The n-th best of the first 256 entries bounds the n-th of all from below (of more where that leaves it at -inf: most beams at rest);
+        // what reaches it is mostly few enough to be ranked at once, each against all.
+        Cand mine = entry(e0);
+        float bound = sort_lanes(__double2float_rd(mine.score));
+        heads[wave][lane] = bound;
+        if (threadIdx.x == 0) few = 0;
+        for (int i = threadIdx.x; i < kRanked; i += blockDim.x) rank_of[i] = 0;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll 1
+            for (int w = 1; w < waves; ++w) {
+                bound = merge_lanes(bound, heads[w][63 - lane]);
+                if (w >= 3 && __shfl(bound, n - 1) > PC_NEG_INF_F) break;
             }
-            if (b == wave) mine = c;
-            else mine = merge_lanes(mine, Cand{__shfl(c.score, 63 - lane), (uint32_t)__shfl((int)c.place, 63 - lane), __shfl(c.token, 63 - lane)});
+            if (lane == n - 1) least = bound;
+        }
+        __syncthreads();
+        Cand *const some = lists[0];
+        for (int e = e0; e < n_entries; e += 64 * waves) {
+            if (e != e0) mine = entry(e);
+            if (mine.beam < PC_MAX_BEAMS && mine.score >= (double)least) {
+                const int at = atomicAdd(&few, 1);
+                if (at < kRanked) some[at] = mine;
+            }
+        }
+        __syncthreads();
+        const int n_some = few;
+        if (n_some <= kRanked) {
+            // candidate i against every parts-th other
+            const int parts = max(1, (int)blockDim.x / n_some), part = threadIdx.x / n_some;
+            for (int i = part < parts ? threadIdx.x % n_some : n_some; i < n_some; i += parts > 1 ? n_some : blockDim.x) {
+                const Cand c = some[i];
+                int rank = 0;
+                for (int j = parts > 1 ? part : 0; j < n_some; j += parts) rank += better(some[j], c);
+                if (rank) atomicAdd(&rank_of[i], rank);
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < n_some; i += blockDim.x)
+                if (rank_of[i] < n) {
+                    const Cand c = some[i];
+                    const int64_t at = g * n + rank_of[i];
+                    out_scores[at] = (float)c.score;
+                    parents[at] = c.beam;
+                    tokens[at] = (int32_t)~(uint32_t)c.key;
+                }
+            __syncthreads();                           // LDS is read
+            continue;
+        }
+        // Many ties, or beams at rest: 64 entries at a time to a wave, which sorts and merges what is better than the n-th best it has; last the
+        // waves' lists, half of them at a time.
+        __syncthreads();
+        mine = none;
+        Cand nth = none;
+        for (int at = 0; at < n_entries; at += 64 * waves) {
+            Cand c = entry(at + e0);
+            if (!__any(better(c, nth))) continue;
+            c = sort_candidates(c);
+            mine = at == 0 ? c : merge_candidates(mine, lane_of(c, 63 - lane));
+            nth = lane_of(mine, n - 1);
         }
         for (int half = waves; half > 1;) {
             const int keep = (half + 1) / 2;
             __syncthreads();
             if (wave >= keep && wave < half) lists[wave][lane] = mine;
             __syncthreads();
-            if (wave + keep < half) mine = merge_lanes(mine, lists[wave + keep][63 - lane]);
+            if (wave + keep < half) mine = merge_candidates(mine, lists[wave + keep][63 - lane]);
             half = keep;
         }
         if (wave == 0 && lane < n) {
             out_scores[g * n + lane] = (float)mine.score;
-            parents[g * n + lane] = (int32_t)(mine.place >> 8);
-            tokens[g * n + lane] = mine.token;
+            parents[g * n + lane] = mine.beam;
+            tokens[g * n + lane] = (int32_t)~(uint32_t)mine.key;
         }
+        __syncthreads();                               // LDS is read
     }
 }
 
-struct StatesDev {
-    int32_t n;
-    pc_state s[PC_MAX_STATES];
+// A state's rows in units of the widest size that suits its addresses, strides and length; its tasks are workgroups: several rows, or
+// part of one.
+constexpr int kCopyUnits = 4;                          // a thread's units, all read before the first is written
+struct CopyTask {
+    const char *src;
+    char *dst;
+    int64_t src_stride, dst_stride, units;             // units of a row
+    int32_t unit, rows, parts;                         // bytes of a unit; rows of a task (1 where a row has several parts); parts of a row
+    int64_t tasks;
 };
+struct CopyTasks { CopyTask t[PC_MAX_STATES]; };
 
-// One workgroup a surviving row and state; bytes.
-__global__ __launch_bounds__(256) void k_beam_reorder(const StatesDev st, const int32_t *__restrict__ parents, int64_t rows, int32_t beams, int32_t n_out)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename U>
+__device__ inline void copy_units(const CopyTask &s, int64_t task, const int32_t *__restrict__ parents, int64_t rows, int32_t beams, int32_t n_out)
 {
-    const pc_state s = st.s[blockIdx.y];
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const int32_t p = parents[r];
-        if (p < 0 || p >= beams) continue;
-        const char *src = (const char *)s.src + (r / n_out * beams + p) * s.src_stride;
-        char *dst = (char *)s.dst + r * s.dst_stride;
-        for (int64_t i = threadIdx.x; i < s.row_bytes; i += 256) dst[i] = src[i];
+    // unit u of row r: with several rows a task, threads go along a row's units and then to the next row
+    const int units = (int)min(s.units, (int64_t)256 * kCopyUnits);
+    U held[kCopyUnits];
+    int64_t to[kCopyUnits];
+#pragma unroll
+    for (int k = 0; k < kCopyUnits; ++k) {
+        const int t = threadIdx.x + 256 * k;
+        const int64_t r = s.parts > 1 ? task / s.parts : task * s.rows + t / units;
+        const int64_t u = s.parts > 1 ? task % s.parts * (256 * kCopyUnits) + t : t % units;
+        const bool on = r < rows && u < s.units && (s.parts > 1 || t < s.rows * units);
+        const int32_t p = parents[on ? r : 0];
+        const bool copied = on && p >= 0 && p < beams;
+        to[k] = copied ? r * s.dst_stride + u * (int64_t)sizeof(U) : -1;
+        held[k] = *reinterpret_cast<const U *>(s.src + (copied ? (r / n_out * beams + p) * s.src_stride + u * (int64_t)sizeof(U) : 0));
+    }
+#pragma unroll
+    for (int k = 0; k < kCopyUnits; ++k)
+        if (to[k] >= 0) *reinterpret_cast<U *>(s.dst + to[k]) = held[k];
+}
+__global__ __launch_bounds__(256) void k_beam_reorder(const CopyTasks states, const int32_t *__restrict__ parents, int64_t rows, int32_t beams, int32_t n_out)
+{
+    const CopyTask &s = states.t[blockIdx.y];
+    for (int64_t task = blockIdx.x; task < s.tasks; task += gridDim.x) {
+        if (s.unit == 16) copy_units<u32x4>(s, task, parents, rows, beams, n_out);
+        else if (s.unit == 4) copy_units<uint32_t>(s, task, parents, rows, beams, n_out);
+        else copy_units<uint8_t>(s, task, parents, rows, beams, n_out);
     }
 }
 
@@ -410,11 +511,12 @@ static pc_status check_beam(const pc_beam *a)
 struct Segments { int32_t n, len; };
 static Segments segments_of(const pc_beam *a)
 {
-    const int64_t rows = (int64_t)a->groups * a->beams, len = (int64_t)a->n_cats + 7, chunks = (len + kChunk - 1) / kChunk;
-    const int64_t most = (1 << 30) / kChunk;           // chunks of a segment whose length is an int32
+    const int64_t chunk = a->scores_type == PC_F32 ? chunk_elements<float>() : chunk_elements<bf16_t>();
+    const int64_t rows = (int64_t)a->groups * a->beams, len = (int64_t)a->n_cats + 7, chunks = (len + chunk - 1) / chunk;
+    const int64_t most = (1 << 30) / chunk;            // chunks of a segment whose length is an int32
     const int64_t wanted = std::min(chunks, std::max(1024 / std::max<int64_t>(rows, 1), (chunks + most - 1) / most));
-    const int64_t each = (chunks + wanted - 1) / wanted;
-    return Segments{(int32_t)((chunks + each - 1) / each), (int32_t)(each * kChunk)};
+    const int64_t each = (chunks + wanted - 1) / std::max<int64_t>(wanted, 1);
+    return Segments{(int32_t)((chunks + each - 1) / each), (int32_t)(each * chunk)};
 }
 static size_t best_bytes(const pc_beam *a) { return ((size_t)a->groups * a->beams * segments_of(a).n * a->n_out * 8 + 15) / 16 * 16; }
 
@@ -450,8 +552,10 @@ pc_status pc_beam_select(const pc_beam *a, void *workspace, size_t workspace_byt
     const hipStream_t s = (hipStream_t)stream;
     const unsigned tasks = (unsigned)std::min<int64_t>((int64_t)a->groups * a->beams * seg.n, 1 << 20);
     with_type(a->scores_type, [&](auto t) { hipLaunchKernelGGL((k_beam_rows<decltype(t)>), dim3(tasks), dim3(kBeamThreads), 0, s, dev, seg.n, seg.len, best, parts); });
-    hipLaunchKernelGGL(k_beam_join, dim3((unsigned)std::min(a->groups, 1 << 20)), dim3((unsigned)(64 * std::min(a->beams, kJoinWaves))), 0, s, dev, seg.n, best,
-                       parts, out_scores, parents, tokens);
+    // a wave for each 64 entries of the lists and for each beam, up to sixteen
+    const int64_t join_waves = std::min<int64_t>(std::max<int64_t>(((int64_t)a->beams * seg.n * a->n_out + 63) / 64, a->beams), kJoinWaves);
+    hipLaunchKernelGGL(k_beam_join, dim3((unsigned)std::min(a->groups, 1 << 20)), dim3((unsigned)(64 * join_waves)), 0, s, dev, seg.n, best, parts, out_scores,
+                       parents, tokens);
     return launched();
 }
 
@@ -461,7 +565,8 @@ pc_status pc_beam_reorder(const pc_state *states, int32_t n_states, const int32_
     if (groups < 0 || beams < 1 || beams > PC_MAX_BEAMS || n_out < 1 || n_out > PC_MAX_BEAM_OUT) return fail(PC_ERR_ARG, "groups, beams or n_out out of range");
     const int64_t rows = (int64_t)groups * n_out, src_rows = (int64_t)groups * beams;
     if (rows > INT32_MAX || src_rows > INT32_MAX) return fail(PC_ERR_TOO_LARGE, "more than 2^31 - 1 rows");
-    StatesDev dev{n_states, {}};
+    CopyTasks dev{};
+    int64_t most = 1;
     struct Span { uintptr_t at, end; };
     Span span[2 * PC_MAX_STATES];
     for (int32_t i = 0; i < n_states; ++i) {
@@ -471,7 +576,13 @@ pc_status pc_beam_reorder(const pc_state *states, int32_t n_states, const int32_
         if (!s.src || !s.dst) return fail(PC_ERR_ARG, "NULL argument");
         span[2 * i] = {(uintptr_t)s.src, (uintptr_t)s.src + (uintptr_t)((src_rows - 1) * s.src_stride + s.row_bytes)};
         span[2 * i + 1] = {(uintptr_t)s.dst, (uintptr_t)s.dst + (uintptr_t)((rows - 1) * s.dst_stride + s.row_bytes)};
-        dev.s[i] = s;
+        const uint64_t at = (uintptr_t)s.src | (uintptr_t)s.dst | (uint64_t)s.row_bytes | (uint64_t)s.src_stride | (uint64_t)s.dst_stride;
+        const int32_t unit = at % 16 == 0 ? 16 : at % 4 == 0 ? 4 : 1;
+        const int64_t units = s.row_bytes / unit, per = 256 * kCopyUnits, parts = (units + per - 1) / per, fit = parts > 1 ? 1 : per / units;
+        if (parts > INT32_MAX) return fail(PC_ERR_TOO_LARGE, "a row of more than 2^31 - 1 parts");
+        dev.t[i] = CopyTask{(const char *)s.src, (char *)s.dst, s.src_stride, s.dst_stride, units, unit, (int32_t)fit, (int32_t)parts,
+                            parts > 1 ? rows * parts : (rows + fit - 1) / fit};
+        most = std::max(most, dev.t[i].tasks);
     }
     if (groups == 0) return PC_OK;
     if (!parents) return fail(PC_ERR_ARG, "NULL argument");
@@ -481,8 +592,8 @@ pc_status pc_beam_reorder(const pc_state *states, int32_t n_states, const int32_
             const Span &d = span[2 * i + 1], &o = span[j];
             if (j != 2 * i + 1 && d.at < o.end && o.at < d.end) return fail(PC_ERR_ARG, "dst overlaps a src or another dst");
         }
-    hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)std::min<int64_t>(rows, 1 << 20), (unsigned)n_states), dim3(256), 0, (hipStream_t)stream, dev, parents,
-                       rows, beams, n_out);
+    hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)std::min<int64_t>(most, 1 << 20), (unsigned)n_states), dim3(256), 0, (hipStream_t)stream, dev, parents, rows,
+                       beams, n_out);
     return launched();
 }
 

@@ -105,6 +105,38 @@ def test_orders_of_a_row_and_ties(order, dtype, V, n):
     check(z[:1], running[:, :1], min(n, V), pad=1)
 
 
+@pytest.mark.parametrize("order", ["ascending", "descending", "constant", "steps", "random", "peaks_last", "mostly_excluded", "all_excluded", "late_excluded"])
+@pytest.mark.parametrize("dtype,V", [("f32", 20011), ("bf16", 33001), ("f16", 17003)])
+@pytest.mark.parametrize("n", [5, 64])
+def test_rows_that_one_workgroup_walks_through(order, dtype, V, n):
+    """So many rows that each is one segment of several chunks; the same four rows in every group, at every alignment."""
+    i = np.arange(V, dtype=np.float64)
+    row = {"ascending": i / V, "descending": -i / V, "constant": 0 * i + 0.5, "steps": np.floor(i / 3000), "random": np.random.default_rng(3).normal(size=V) * 3,
+           "peaks_last": np.where(i > V - 40, i, 0.0), "mostly_excluded": np.where(i % 4999 == 17, i / V, -np.inf), "all_excluded": np.full(V, -np.inf),
+           "late_excluded": np.where(i < V - 3, -np.inf, i / V)}[order]
+    four = torch.from_numpy(np.stack([row, row[::-1].copy(), np.roll(row, V // 2), row])).to(TYPES[dtype])
+    G = 300                                                 # 1200 rows
+    running = torch.tensor([[-0.5, -0.25, -1.0, -0.5]])
+    got = select(four.repeat(G, 1), running.repeat(G, 1), n, pad=1)
+    scores, parents, tokens, _ = reference(four, running, n)
+    for g in (got[1] != parents, got[2] != tokens, got[0] != scores.astype(np.float32)):
+        assert not g.any()
+
+
+@pytest.mark.parametrize("live", [0, 1, 2, 40])
+@pytest.mark.parametrize("V", [64, 9000])
+def test_many_beams_of_which_few_live(live, V):
+    """64 beams and survivors: 4096 entries to join, most or all of them at -inf."""
+    z, running, rng = draw(2, 64, V, "f32", 61)
+    running[:, live:] = -float("inf")
+    done = np.zeros((2, 64), np.uint8)
+    done[1, ::2] = 1
+    for n in (1, 64):
+        check(z, running, n)
+        check(z, running, n, done=done, done_token=V - 1)
+        check(torch.zeros_like(z), torch.zeros_like(running), n)    # every candidate ties
+
+
 def test_signed_zeros_tie_and_numbers_that_are_none_come_last():
     inf, nan = float("inf"), float("nan")
     z = torch.tensor([[-0.0, 0.0, -0.0, nan, -inf, 1.0, nan, -1.0], [inf, inf, 0.0, -inf, nan, -inf, 2.0, inf]])
