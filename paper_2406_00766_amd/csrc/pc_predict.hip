@@ -399,7 +399,6 @@ __device__ inline void flow_column(const pc_mixture &m, int n, int64_t &w_at, in
     o_at = blk.row >= 0 ? (int64_t)blk.table * m.n_cats * m.K + n % m.K : 0;      // a place that exists
     more = again;
 }
-__device__ inline bool aligned_weights(const pc_mixture &m) { return m.stride % 4 == 0 && ((uintptr_t)m.weights & 15) == 0; }
 
 // Table flows.  A workgroup of 2 x 2 waves owns a tile of 64 IC categories x 64 IN columns, a column being a node of a block.  The samples are
 // added up 16 at a time from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six
@@ -430,7 +429,6 @@ __global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_
     if (c0 >= m.n_cats) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int cw = wave / 2 * 32 * IC, nw = wave % 2 * 32 * IN;
-    const bool vec = aligned_weights(m);
     for (int i = threadIdx.x; i < TN; i += TH) flow_column(m, n0 + i, w_at[i], o_at[i], more[i]);
     __syncthreads();
     // What a thread stages a step: eight samples of a category (the group of samples is the wave's), and of a column (two lanes read 16 samples
@@ -533,9 +531,10 @@ __global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_
         };
         auto eight = [&](const float *row, int i0, float (&x)[8]) {
             const int i = i0 + 8 * w_group;
-            if (all && vec && i0 + 16 <= n_samples) {
-                const float4 u = *reinterpret_cast<const float4 *>(row + s0 + i), v = *reinterpret_cast<const float4 *>(row + s0 + i + 4);
-                x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+            if (all && i0 + 16 <= n_samples) {
+                const Pack<float> u = load_pack(row + s0 + i), v = load_pack(row + s0 + i + 4);      // a row may begin at any float
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { x[e] = u.v[e]; x[4 + e] = v.v[e]; }
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = row[sample(min(i + e, n_samples - 1))];
@@ -740,8 +739,9 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     if (logp_ld < m->n_cats || dlogp_ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4) || !aligned_to(dlogp, 4)) return fail(PC_ERR_ARG, "logp and dlogp must be 4-byte aligned");
     if (!aligned_to(table_flow, 16)) return fail(PC_ERR_ARG, "table_flow must be 16-byte aligned");
-    // Tiles: 128 x 256 for many samples, 128 x 128 for fewer (a third workgroup a CU reads and writes: 4096 states x 50257, B = 32 410 us against 466,
-    // B = 256 1161 against 981), where they give every CU two; else 64 x 64.  Looking for samples to leave out pays from some 128 on.
+    // Tiles: of very many, 128 x 256 from 128 samples on and 128 x 128 below (4096 states x 50257: B = 32 393 us against 466, B = 256 1161 against
+    // 981; by 64 x 64 412 at B = 32); of fewer, which such tiles would cover in two or three rounds of workgroups, 64 x 64 (512 states: B = 16
+    // 58 us against 86, B = 96 97 against 112).  Looking for samples to leave out pays from some 128 on.
     const int64_t H = (int64_t)m->n_blocks * m->K;
     const auto tiles = [&](int64_t tc, int64_t tn) { return ((m->n_cats + tc - 1) / tc + 7) / 8 * 8 * ((H + tn - 1) / tn); };
     const hipStream_t s = (hipStream_t)stream;
@@ -749,9 +749,13 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
 #define PC_FLOW(IC, IN, SCAN)                                                                                                              \
     hipLaunchKernelGGL((m->table ? k_predict_flow<IC, IN, SCAN, true> : k_predict_flow<IC, IN, SCAN, false>), dim3((unsigned)tiles(64 * IC, 64 * IN)), dim3(256), 0, \
                        s, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale, accumulate, table_flow)
-    if (tiles(128, 256) >= 512 && B >= 128) PC_FLOW(2, 4, true);
-    else if (tiles(128, 128) >= 512) PC_FLOW(2, 2, false);
-    else PC_FLOW(1, 1, false);
+    if (tiles(128, 128) >= 4096) {
+        if (B >= 128) PC_FLOW(2, 4, true);
+        else PC_FLOW(2, 2, false);
+    } else {
+        if (B >= 128) PC_FLOW(1, 1, true);
+        else PC_FLOW(1, 1, false);
+    }
 #undef PC_FLOW
     return launched();
 }
