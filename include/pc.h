@@ -272,8 +272,10 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
  * which is the objective's gradient with respect to log tables[t][c][k];  table_flow = scale * flow for the tables that the mixture
  * names, added to what is there where `accumulate` is set.  With dlogp = -q (a loss -sum q logp, q >= 0) and scale = -1 these are
  * the flows of an EM step on soft targets, ready for pc_em_step.  Entries of logp below log FLT_MIN add nothing. */
+pc_status pc_predict_backward_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t B, const float *logp, int64_t logp_ld,
-                              const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow, void *stream);
+                              const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow,
+                              void *workspace, size_t workspace_bytes, void *stream);
 
 /* Distillation from a teacher's top logits.  Per row, with temperature T:
  *   q_j  = softmax over the listed entries of teacher_j / T, or exp(teacher_j / T - teacher_lse) where the teacher's own

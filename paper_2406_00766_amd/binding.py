@@ -89,8 +89,9 @@ EXPORTS = ["pc_compile", "pc_compile_host", "pc_destroy", "pc_last_error", "pc_g
            "pc_forward_static", "pc_backward", "pc_em_step", "pc_profile_enable", "pc_profile_read", "pc_kernel_class_name",
            "pc_measure_copy", "pc_measure_mfma_f32", "pc_collapse", "pc_collapsed_dag", "pc_collapsed_theta",
            "pc_collapsed_block_map", "pc_collapsed_destroy", "pc_order_for_scratch", "pc_set_wait_limit",
-           "pc_get_mixture", "pc_predict", "pc_predict_backward", "pc_distill_workspace_bytes", "pc_distill_forward",
-           "pc_distill_backward", "pc_beam_workspace_bytes", "pc_beam_select", "pc_beam_reorder"]
+           "pc_get_mixture", "pc_predict", "pc_predict_backward_workspace_bytes", "pc_predict_backward",
+           "pc_distill_workspace_bytes", "pc_distill_forward", "pc_distill_backward", "pc_beam_workspace_bytes",
+           "pc_beam_select", "pc_beam_reorder"]
 
 _lib = None
 
@@ -143,7 +144,8 @@ def lib():
         L.pc_get_mixture.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(pc_mixture)]
         L.pc_predict.argtypes = [C.POINTER(pc_mixture), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
         L.pc_predict_backward.argtypes = [C.POINTER(pc_mixture), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
-                                          C.c_float, C.c_int32, C.c_void_p, C.c_void_p]
+                                          C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.pc_predict_backward_workspace_bytes.argtypes = [C.POINTER(pc_mixture), C.c_int32, C.POINTER(C.c_size_t)]
         L.pc_distill_workspace_bytes.argtypes = [C.POINTER(pc_distill), C.POINTER(C.c_size_t)]
         L.pc_distill_forward.argtypes = [C.POINTER(pc_distill), C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
         L.pc_distill_backward.argtypes = [C.POINTER(pc_distill), C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]
@@ -488,8 +490,15 @@ def pc_predict(m: mixture, tables, B, logp, stream=None):
     _call(m.index, stream, lib().pc_predict, C.byref(s), tables.data_ptr(), B, *out)
 
 
-def pc_predict_backward(m: mixture, tables, B, logp, dlogp, scale, table_flow, accumulate=True, stream=None):
-    """Table flows for a gradient dlogp [B, n_cats] of an objective; added to table_flow, or stored."""
+def pc_predict_backward_workspace_bytes(m: mixture, B) -> int:
+    n = C.c_size_t()
+    _check(lib().pc_predict_backward_workspace_bytes(C.byref(m.struct), int(B), C.byref(n)))
+    return int(n.value)
+
+
+def pc_predict_backward(m: mixture, tables, B, logp, dlogp, scale, table_flow, accumulate=True, stream=None, workspace=None):
+    """Table flows for a gradient dlogp [B, n_cats] of an objective; added to table_flow, or stored.  workspace: a uint8 tensor of
+    pc_predict_backward_workspace_bytes; None: one is allocated on the call's stream."""
     import torch
     s, B = m.struct, int(B)
     n = s.n_tables * s.n_cats * s.K
@@ -498,8 +507,17 @@ def pc_predict_backward(m: mixture, tables, B, logp, dlogp, scale, table_flow, a
     if B > m.columns:
         _refuse("weights have fewer than B columns")
     shape = (B, s.n_cats)
-    _call(m.index, stream, lib().pc_predict_backward, C.byref(s), tables.data_ptr(), B, *_rows("logp", logp, torch.float32, shape, m.index),
-          *_rows("dlogp", dlogp, torch.float32, shape, m.index), float(scale), 1 if accumulate else 0, table_flow.data_ptr())
+    args = (*_rows("logp", logp, torch.float32, shape, m.index), *_rows("dlogp", dlogp, torch.float32, shape, m.index))
+    if workspace is None:
+        size = pc_predict_backward_workspace_bytes(m, B)
+        if size:
+            if stream is None:
+                workspace = torch.empty(size, dtype=torch.uint8, device=m.index)
+            else:                                       # memory of the stream that uses it: freed, it serves that stream's later work only
+                with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=m.index) if isinstance(stream, int) else stream):
+                    workspace = torch.empty(size, dtype=torch.uint8, device=m.index)
+    _call(m.index, stream, lib().pc_predict_backward, C.byref(s), tables.data_ptr(), B, *args, float(scale), 1 if accumulate else 0,
+          table_flow.data_ptr(), *_workspace(workspace, m.index))
 
 
 class distill:

@@ -24,7 +24,7 @@ __device__ inline MixBlock mix_block(const pc_mixture &m, int j)
 
 constexpr float kLogFltMin = -87.33654475f;           // log FLT_MIN
 
-// 64 categories x 64 samples a workgroup, 4 x 4 sums a thread, the states in steps of 16 through LDS.  Any K.
+// K below 4.  64 categories x 64 samples a workgroup, 4 x 4 sums a thread, the states in steps of 16 through LDS.
 __global__ __launch_bounds__(256) void k_predict_any(const pc_mixture m, const float *__restrict__ tables, int32_t B,
                                                      float *__restrict__ logp, int64_t ld)
 {
@@ -61,7 +61,12 @@ __global__ __launch_bounds__(256) void k_predict_any(const pc_mixture m, const f
             }
 }
 
-// ---- matrix-core kernels: K a multiple of 4 ----
+// ---- matrix-core kernels: K of at least 4 ----
+// States come in groups of four that begin where 16 bytes of a block can be read: a block's last group is its last four states, and where K is
+// no multiple of 4 the `skip` weights that the group before has counted are taken as zero.
+__device__ inline int group_states(int K) { return (K + 3) & ~3; }      // of a block, with those repeated
+__device__ inline int group_start(int K, int k) { return min(k, K - 4); }
+
 // Operands are fp32; the matrix cores multiply bf16 and add in fp32.  An operand x is taken as a sum of bf16 planes, each the rounding of
 // what the planes before it leave: hi + lo keeps 2^-16 of x, hi + mid + lo 2^-24.  Weights (and tables) are scaled by 2^24 on the way, so that the
 // lower planes of numbers down to FLT_MIN are normal numbers; the scale is taken out of the fp32 sum, exactly.
@@ -115,7 +120,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     __shared__ uint4 planes[2][PLANES][KW / 8][NB];   // [buffer][plane][8 states][sample]
     __shared__ int64_t t_at[kWindow / 4], w_at[kWindow / 4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5, part = wave % SPLIT;
-    const int H = m.n_blocks * m.K, c0 = (blockIdx.x * (WAVES / SPLIT) + wave / SPLIT) * 32, b0 = blockIdx.y * NB;
+    const int Kg = group_states(m.K), H = m.n_blocks * Kg, c0 = (blockIdx.x * (WAVES / SPLIT) + wave / SPLIT) * 32, b0 = blockIdx.y * NB;
     const int64_t mine = (int64_t)min(c0 + col, m.n_cats - 1) * m.K;     // a category behind the last reads that one's row again
     const int here = min(NB, B - b0);                  // samples of this workgroup
     floatx16 acc[NT];
@@ -138,16 +143,18 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     auto fill_window = [&](int n0) {
         for (int i = threadIdx.x; i < kWindow / 4; i += TH) {
             const int n = n0 + 4 * i;
-            const MixBlock blk = n < H ? mix_block(m, n / m.K) : MixBlock{-1, -1};
-            t_at[i] = blk.row >= 0 ? (int64_t)blk.table * m.n_cats * m.K + n % m.K : -1;
-            w_at[i] = blk.row >= 0 ? (blk.row + n % m.K) * m.stride : -1;
+            const MixBlock blk = n < H ? mix_block(m, n / Kg) : MixBlock{-1, -1};
+            const int k = group_start(m.K, n % Kg);
+            t_at[i] = blk.row >= 0 ? (int64_t)blk.table * m.n_cats * m.K + k : -1;
+            w_at[i] = blk.row >= 0 ? (blk.row + k) * m.stride * 4 + (n % Kg - k) : -1;      // and how many to skip
         }
     };
     // What lies outside (blocks left out, states behind the last, samples behind B) is read from a place that exists and masked when it is
     // split.  A chunk behind the last state is fetched and staged like any other, and not used.
-    float4 t_raw[STEPS][2];
+    Pack<float> t_raw[STEPS][2];
     float w_raw[FT][8];
-    uint32_t t_mask[WHOLE ? 1 : STEPS][2], w_mask[FT][2];
+    uint32_t t_mask[WHOLE ? 1 : STEPS][2];
+    int w_skip[FT][2];                                 // 4: all
     auto fetch_weights = [&](int n0, int f) {          // of the chunk that begins with state n0
         const int g0 = n0 % kWindow / 4;
         if (!wave_stages[f]) return;
@@ -155,8 +162,8 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const int64_t at = task_g[f] >= 0 && task_b[f] < here ? w_at[g0 + 2 * task_g[f] + q] : -1;
-            const float *src = m.weights + (at >= 0 ? at : 0) + b0 + b;
-            w_mask[f][q] = at >= 0 ? ~0u : 0u;
+            const float *src = m.weights + (at >= 0 ? at >> 2 : 0) + b0 + b;
+            w_skip[f][q] = at >= 0 ? (int)at & 3 : 4;
 #pragma unroll
             for (int i = 0; i < 4; ++i) w_raw[f][4 * q + i] = src[i * m.stride];
         }
@@ -171,7 +178,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int q = 0; q < 2; ++q) t_raw[s][q] = *reinterpret_cast<const float4 *>(src + 16 * s + 4 * q);
+                for (int q = 0; q < 2; ++q) t_raw[s][q] = load_pack(src + 16 * s + 4 * q);
         } else {
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
                 for (int q = 0; q < 2; ++q) {
                     const int64_t at = t_at[g0 + part * (KC / 4) + 4 * s + 2 * half + q];
                     t_mask[s][q] = at >= 0 ? ~0u : 0u;
-                    t_raw[s][q] = *reinterpret_cast<const float4 *>(tables + (at >= 0 ? at : 0) + mine);
+                    t_raw[s][q] = load_pack(tables + (at >= 0 ? at : 0) + mine);
                 }
         }
     };
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
         float x[8];
         uint4 pl[PLANES];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = masked(w_raw[f][i], w_mask[f][i / 4]);
+        for (int i = 0; i < 8; ++i) x[i] = i % 4 >= w_skip[f][i / 4] ? w_raw[f][i] * kUp : 0.0f;
         split8(x, pl);
         if (NT > 1 || task_g[f] >= 0)
 #pragma unroll
@@ -197,9 +204,9 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     };
     uint4 tp[STEPS][PLANES];
     auto split_tables = [&](int s) {
-        const float4 u = t_raw[s][0], v = t_raw[s][1];
-        const uint32_t m0 = t_mask[WHOLE ? 0 : s][0], m1 = t_mask[WHOLE ? 0 : s][WHOLE ? 0 : 1];
-        const float x[8] = {masked(u.x, m0), masked(u.y, m0), masked(u.z, m0), masked(u.w, m0), masked(v.x, m1), masked(v.y, m1), masked(v.z, m1), masked(v.w, m1)};
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = masked(t_raw[s][i / 4].v[i % 4], t_mask[WHOLE ? 0 : s][WHOLE ? 0 : i / 4]);
         split8(x, tp[s]);
     };
 
@@ -303,9 +310,9 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
 {
     __shared__ float4 w[kFewFloats / 4];              // [block of the window][sample][piece]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int P = m.K / 4, R = 64 / P, piece = lane % P, r = lane / P;      // pieces of a row, rows of an instruction
+    const int P = group_states(m.K) / 4, R = 64 / P, piece = lane % P, r = lane / P;      // pieces of a row, rows of an instruction
     const bool idle = r >= R;
-    const int per_window = min(m.n_blocks, kFewFloats / (NS * m.K));        // at least 16: K <= 128, NS <= 2
+    const int per_window = min(m.n_blocks, kFewFloats / (NS * 4 * P));      // at least 16: K <= 128, NS <= 2
     const int64_t c0 = ((int64_t)blockIdx.x * 4 + wave) * R * kFewRows + (idle ? 0 : r);
     float acc[kFewRows][NS];
     bool on[2];
@@ -315,7 +322,7 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
         for (int s = 0; s < NS; ++s) acc[u][s] = 0.0f;
     int64_t row[kFewRows];                                 // a category behind the last reads that one's row again
 #pragma unroll
-    for (int u = 0; u < kFewRows; ++u) row[u] = min(c0 + u * R, (int64_t)m.n_cats - 1) * m.K + 4 * piece;
+    for (int u = 0; u < kFewRows; ++u) row[u] = min(c0 + u * R, (int64_t)m.n_cats - 1) * m.K + group_start(m.K, 4 * piece);
     for (int j0 = 0; j0 < m.n_blocks; j0 += per_window) {
         const int here = min(per_window, m.n_blocks - j0);
         __syncthreads();
@@ -324,19 +331,20 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
             const MixBlock blk = mix_block(m, j0 + j);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (blk.row >= 0 && b < B) {
-                const float *src = m.weights + (blk.row + 4 * q) * m.stride + b;
-                v = make_float4(src[0], src[m.stride], src[2 * m.stride], src[3 * m.stride]);
+                const int k = group_start(m.K, 4 * q), skip = 4 * q - k;
+                const float *src = m.weights + (blk.row + k) * m.stride + b;
+                v = make_float4(skip > 0 ? 0.f : src[0], skip > 1 ? 0.f : src[m.stride], skip > 2 ? 0.f : src[2 * m.stride], src[3 * m.stride]);
             }
             w[(j * NS + b) * P + q] = v;
         }
         __syncthreads();
-        float4 t[2][kFewRows];                             // a block's rows, while those of the one before are added up
+        Pack<float> t[2][kFewRows];                             // a block's rows, while those of the one before are added up
         auto fetch = [&](int j, int set) {             // a block left out reads the first table's rows and is not added
             const MixBlock blk = mix_block(m, j0 + j);
             on[set] = blk.row >= 0;
             const float *src = tables + (int64_t)max(blk.table, 0) * m.n_cats * m.K;
 #pragma unroll
-            for (int u = 0; u < kFewRows; ++u) t[set][u] = *reinterpret_cast<const float4 *>(src + row[u]);
+            for (int u = 0; u < kFewRows; ++u) t[set][u] = load_pack(src + row[u]);
         };
         auto add = [&](int j, int set) {
             if (!on[set]) return;
@@ -344,7 +352,7 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
             for (int s = 0; s < NS; ++s) {
                 const float4 v = w[(j * NS + s) * P + piece];
 #pragma unroll
-                for (int u = 0; u < kFewRows; ++u) acc[u][s] += t[set][u].x * v.x + t[set][u].y * v.y + t[set][u].z * v.z + t[set][u].w * v.w;
+                for (int u = 0; u < kFewRows; ++u) acc[u][s] += t[set][u].v[0] * v.x + t[set][u].v[1] * v.y + t[set][u].v[2] * v.z + t[set][u].v[3] * v.w;
             }
         };
         fetch(0, 0);
@@ -372,14 +380,15 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
     }
 }
 
-// g / p of one sample and category; p = 0 adds nothing.  exp(-logp) as 2^t times what t = -logp log2(e), rounded, leaves out: good to 2^-23 over the
+// 2^-24 g / p of one sample and category (the weights are scaled by 2^24: a weight times g / p, which may be as large as g over the smallest
+// table entry, stays what it is); p = 0 adds nothing.  exp(-logp) as 2^t times what t = -logp log2(e), rounded, leaves out: good to 2^-23 over the
 // whole range, for half the instructions of expf.
 __device__ inline float flow_ratio(float logp, float g)
 {
     constexpr float kLog2e = 1.44269504f, kRest = 1.92596299e-8f, kLn2 = 0.693147181f;    // log2(e) = kLog2e + kRest
     const float t = -logp * kLog2e, rest = fmaf(-logp, kRest, fmaf(-logp, kLog2e, -t));
     const float e = __builtin_amdgcn_exp2f(t);
-    return logp < kLogFltMin - 1e-3f ? 0.0f : g * fmaf(e, rest * kLn2, e);
+    return logp < kLogFltMin - 1e-3f ? 0.0f : (g * kDown) * fmaf(e, rest * kLn2, e);
 }
 
 // Column n of the flows: its first weight (-1: none, or another block's column does its table's work), its place in the flows for category 0,
@@ -400,115 +409,125 @@ __device__ inline void flow_column(const pc_mixture &m, int n, int64_t &w_at, in
     more = again;
 }
 
-// Table flows.  A workgroup of 2 x 2 waves owns a tile of 64 IC categories x 64 IN columns, a column being a node of a block.  The samples are
+// What k_predict_flow<MARKED> reads: the weights by sample, wt[b][n], a table's further blocks added to its first one's column, in the
+// first `turns` workgroups, 64 columns x 64 samples each; in the others marks, a wave for 64 categories and 32 samples: bit b % 32 of
+// marks[c / 64][b / 32] is set where sample b has a gradient that is not zero among those categories.
+__global__ __launch_bounds__(256) void k_flow_prepare(const pc_mixture m, int32_t B, const float *__restrict__ dlogp, int64_t ld, int32_t turns, float *__restrict__ wt,
+                                                      uint32_t *__restrict__ marks)
+{
+    __shared__ float x[64][65];
+    __shared__ int64_t w_at[64], o_at[64];
+    __shared__ int32_t more[64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = m.n_blocks * m.K;
+    if ((int)blockIdx.x < turns) {
+        const int n0 = blockIdx.x % ((H + 63) / 64) * 64, b0 = blockIdx.x / ((H + 63) / 64) * 64, b = min(b0 + lane, B - 1);
+        if (wave == 0) flow_column(m, n0 + lane, w_at[lane], o_at[lane], more[lane]);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[wave + 4 * i][lane] = m.weights[max(w_at[wave + 4 * i], (int64_t)0) + b];
+        for (int i = 0; i < 16; ++i) {
+            const int c = wave + 4 * i;
+            if (m.table && w_at[c] >= 0 && more[c])
+                for (int o = (n0 + c) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
+                    const MixBlock blk = mix_block(m, o);
+                    if (blk.row >= 0 && blk.table == t) x[c][lane] += m.weights[(blk.row + (n0 + c) % m.K) * m.stride + b];
+                }
+        }
+        __syncthreads();
+        for (int i = 0; i < 16; ++i) {
+            const int s = wave + 4 * i;
+            if (b0 + s < B && n0 + lane < H) wt[(int64_t)(b0 + s) * H + n0 + lane] = x[lane][s];
+        }
+        return;
+    }
+    const int64_t rows = (m.n_cats + 63ll) / 64, words = (B + 31ll) / 32, job = (int64_t)(blockIdx.x - turns) * 4 + wave;
+    if (job >= rows * words) return;
+    const int64_t row = job % rows, word = job / rows, c = min(row * 64 + lane, (int64_t)m.n_cats - 1);
+    float g[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) g[e] = dlogp[min(word * 32 + e, (int64_t)B - 1) * ld + c];
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) bits |= (__ballot(g[e] != 0.0f) != 0 && word * 32 + e < B ? 1u : 0u) << e;
+    if (lane == 0) marks[row * words + word] = bits;
+}
+
+// Table flows.  A workgroup of 2 x 2 waves owns a tile of 64 I categories x 64 I columns, a column being a node of a block.  The samples are
 // added up 16 at a time from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six
 // products (the terms of a flow have either sign and are few, so that nothing averages out; the fp32 matrix instructions took longer:
-// 4096 states x 50257, B = 256 1372 us).  While a step is multiplied the next one's operands are split and staged and the one after is on its
-// way.  Bound by the matrix cores' sustained rate from some 150 samples on, before by reading the tables and writing their flows, which the
-// products of a CU's other workgroup cover.
-// SCAN: samples whose g is zero for all of the tile's categories are left out (targets of a few categories a sample: an EM step), except
-// where the first 32 of kSegment samples show that few are.
+// 4096 states x 50257, B = 256 1372 us against 1020).  While a step is multiplied the next one's operands are split and staged and the one
+// after is on its way.  Bound by the matrix cores' sustained rate from some 100 samples on (B = 256: six products 557 us), before by reading
+// the tables and writing their flows (B = 32: 389 us, 4.3 TB/s), which the products of a CU's other workgroups cover.
+// MARKED: of every kSegment samples those without gradient among the tile's categories are left out (targets of a few categories a sample:
+// an EM step; 64 categories a sample, B = 256 445 us against 967 with all of them), except where few would be; the weights are those of
+// k_flow_prepare, by sample, so that the columns of any sample are neighbours (gathered from the rows of m.weights: 737 us).
 // LISTS: a table named by several blocks is the first one's: its column adds up all their weights, the others' columns do nothing, so every entry has
 // one writer.  The workgroups of a category tile follow one another on one XCD, whose cache keeps its g / p.
 constexpr int kSegment = 512;
-template <int IC, int IN, bool SCAN, bool LISTS>
-__global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_flow(const pc_mixture m, const float *__restrict__ tables, int32_t B, const float *__restrict__ logp,
+template <int I, bool MARKED, bool LISTS>
+__global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_mixture m, const float *__restrict__ tables, int32_t B, const float *__restrict__ logp,
                                                          int64_t lp_ld, const float *__restrict__ dlogp, int64_t dl_ld, float scale, int32_t accumulate,
-                                                         float *__restrict__ flow)
+                                                         float *__restrict__ flow, const float *__restrict__ wt, const uint32_t *__restrict__ marks)
 {
-    constexpr int TH = 256, WAVES = 4, TC = 64 * IC, TN = 64 * IN, NP = TN + 4;   // four more: the two groups of a column lie in other banks
+    constexpr int TH = 256, TC = 64 * I, TN = 64 * I, NP = TN + 4;   // four more: the two groups of a column lie in other banks
     __shared__ uint4 rs[2][3][2][TC], ws[2][3][2][NP];                            // [buffer][plane][8 samples][category or column]
     __shared__ int64_t w_at[TN], o_at[TN];            // first weight of a column, -1: none; its place in the flows for category 0
     __shared__ int32_t more[TN];                      // the column's table has further blocks
-    __shared__ uint16_t list[SCAN ? kSegment : 1];    // samples of the segment that count
-    __shared__ uint8_t counts[SCAN ? kSegment : 1];
+    __shared__ uint16_t list[MARKED ? kSegment : 1];    // samples of the segment that count
     __shared__ int32_t n_list;
     const int H = m.n_blocks * m.K, n_tiles = (H + TN - 1) / TN, q = blockIdx.x / 8;
     const int64_t c0 = ((int64_t)(q / n_tiles) * 8 + blockIdx.x % 8) * TC;
     const int n0 = q % n_tiles * TN;
     if (c0 >= m.n_cats) return;
+    const int64_t mark_rows = (m.n_cats + 63ll) / 64, mark_ld = (B + 31ll) / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-    const int cw = wave / 2 * 32 * IC, nw = wave % 2 * 32 * IN;
+    const int cw = wave / 2 * 32 * I, nw = wave % 2 * 32 * I;
     for (int i = threadIdx.x; i < TN; i += TH) flow_column(m, n0 + i, w_at[i], o_at[i], more[i]);
     __syncthreads();
     // What a thread stages a step: eight samples of a category (the group of samples is the wave's), and of a column (two lanes read 16 samples
     // of a row).  Categories behind the last and columns without weights repeat others: their sums are not stored.
-    constexpr int WT = IN == 4 ? 2 : 1;               // columns of a thread
-    static_assert((IC == 2 && IN >= 2) || (IC == 1 && IN == 1), "the dealing below");
-    const bool of_ratios = IC == 2 || wave < 2, of_weights = IC == 2 || wave >= 2;
-    const int r_group = IC == 2 ? wave / 2 : wave % 2, r_cat = IC == 2 ? threadIdx.x % TC : lane, w_group = lane % 2;
+    static_assert(I == 1 || I == 2, "the dealing below");
+    const bool of_ratios = I == 2 || wave < 2, of_weights = I == 2 || wave >= 2;
+    const int r_group = I == 2 ? wave / 2 : wave % 2, r_cat = I == 2 ? threadIdx.x % TC : lane;
     const int64_t cat = min(c0 + r_cat, (int64_t)m.n_cats - 1);
-    int w_col[WT];
-    const float *w_row[WT];
-    bool w_more = false;
+    const int w_col = MARKED ? (I == 2 ? threadIdx.x % TN : lane) : threadIdx.x % (I == 2 ? TH : TH / 2) / 2;
+    const int w_group = MARKED ? r_group : lane % 2;
+    const float *w_row = MARKED ? wt + min(n0 + w_col, H - 1) : m.weights + max(w_at[w_col], (int64_t)0);
+    const bool w_more = LISTS && w_at[w_col] >= 0 && more[w_col];
+    floatx16 acc[I][I];
 #pragma unroll
-    for (int f = 0; f < WT; ++f) {
-        w_col[f] = threadIdx.x % (IC == 2 ? TH : TH / 2) / 2 + f * (TH / 2);
-        w_row[f] = m.weights + max(w_at[w_col[f]], (int64_t)0);
-        w_more |= w_at[w_col[f]] >= 0 && more[w_col[f]];
-    }
-    floatx16 acc[IC][IN];
+    for (int i = 0; i < I; ++i)
 #pragma unroll
-    for (int i = 0; i < IC; ++i)
-#pragma unroll
-        for (int k = 0; k < IN; ++k)
+        for (int k = 0; k < I; ++k)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.0f;
     bool none = true;                                  // no sample counts for this tile
-    for (int s0 = 0; s0 < B; s0 += SCAN ? kSegment : B) {
-        const int here = SCAN ? min(kSegment, B - s0) : B;
+    for (int s0 = 0; s0 < B; s0 += MARKED ? kSegment : B) {
+        const int here = MARKED ? min(kSegment, B - s0) : B;
         bool all = true;
-        if (SCAN) {
-            // which samples count: 32 at a time, all categories of the tile, a wave per sample
-            auto look = [&](int from, int to, auto at_once) {
-                constexpr int AT = decltype(at_once)::value;
-                for (int b0 = from + wave * AT; b0 < to; b0 += WAVES * AT) {
-                    float g[AT][IC];
-#pragma unroll
-                    for (int e = 0; e < AT; ++e)
-#pragma unroll
-                        for (int i = 0; i < IC; ++i)
-                            g[e][i] = dlogp[(s0 + min(b0 + e, to - 1)) * dl_ld + min(c0 + lane + 64 * i, (int64_t)m.n_cats - 1)];
-#pragma unroll
-                    for (int e = 0; e < AT; ++e) {
-                        bool any = false;
-#pragma unroll
-                        for (int i = 0; i < IC; ++i) any |= g[e][i] != 0.0f;
-                        const bool on = __ballot(any) != 0;
-                        if (lane == 0 && b0 + e < to) counts[b0 + e] = on;
-                    }
-                }
-            };
-            auto compact = [&](int to) {               // one wave
+        if (MARKED) {                                  // the samples that count, in order
+            __syncthreads();
+            if (wave == 0) {
                 int n = 0;
-                for (int b = 0; b < to; b += 64) {
-                    const bool on = b + lane < to && counts[b + lane];
-                    const uint64_t those = __ballot(on);
-                    if (on) list[n + __popcll(those & ((1ull << lane) - 1))] = (uint16_t)(b + lane);
+                for (int b = 0; b < here; b += 64) {
+                    uint64_t those = 0;
+                    for (int i = 0; i < I; ++i)
+                        for (int h = 0; h < 2; ++h)
+                            if (b + 32 * h < here && c0 / 64 + i < mark_rows)
+                                those |= (uint64_t)marks[(c0 / 64 + i) * mark_ld + (s0 + b) / 32 + h] << 32 * h;
+                    if (those >> lane & 1) list[n + __popcll(those & ((1ull << lane) - 1))] = (uint16_t)(b + lane);
                     n += __popcll(those);
                 }
                 if (lane == 0) n_list = n;
-            };
-            const int few = min(here, 32);
-            __syncthreads();
-            look(0, few, std::integral_constant<int, 8>{});
-            __syncthreads();
-            if (wave == 0) compact(few);
-            __syncthreads();
-            all = n_list * 4 > few * 3;
-            __syncthreads();
-            if (!all && here > few) {
-                look(few, here, std::integral_constant<int, 32>{});
-                __syncthreads();
-                if (wave == 0) compact(here);
-                __syncthreads();
             }
+            __syncthreads();
+            all = n_list * 4 > here * 3;
         }
         const int n_samples = all ? here : n_list;
         if (n_samples == 0) continue;
         none = false;
-        auto sample = [&](int i) { return s0 + (!SCAN || all ? i : list[i]); };
-        float l[8], d[8], w[WT][8];
+        auto sample = [&](int i) { return s0 + (!MARKED || all ? i : list[i]); };
+        float l[8], d[8], w[8];
         auto fetch_ratios = [&](int i0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -529,60 +548,61 @@ __global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_
 #pragma unroll
             for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = pl[p];
         };
-        auto eight = [&](const float *row, int i0, float (&x)[8]) {
-            const int i = i0 + 8 * w_group;
-            if (all && i0 + 16 <= n_samples) {
-                const Pack<float> u = load_pack(row + s0 + i), v = load_pack(row + s0 + i + 4);      // a row may begin at any float
+        auto eight = [&](const float *row, int i, float (&x)[8]) {
+            if (i + 8 <= n_samples) {
+                const Pack<float> u = load_pack(row + i), v = load_pack(row + i + 4);      // a row may begin at any float
 #pragma unroll
                 for (int e = 0; e < 4; ++e) { x[e] = u.v[e]; x[4 + e] = v.v[e]; }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = row[sample(min(i + e, n_samples - 1))];
+                for (int e = 0; e < 8; ++e) x[e] = row[min(i + e, n_samples - 1)];
             }
         };
-        auto fetch_weights = [&](int i0, int f) {
-            eight(w_row[f], i0, w[f]);
-            if (LISTS && w_more && w_at[w_col[f]] >= 0 && more[w_col[f]])
-                for (int o = (n0 + w_col[f]) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
+        auto fetch_weights = [&](int i0) {
+            if (MARKED) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    w[e] = w_row[(int64_t)__builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * w_group + e, n_samples - 1))) * H];
+                return;
+            }
+            eight(w_row, i0 + 8 * w_group, w);
+            if (w_more)
+                for (int o = (n0 + w_col) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
                     const MixBlock blk = mix_block(m, o);
                     if (blk.row < 0 || blk.table != t) continue;
                     float y[8];
-                    eight(m.weights + (blk.row + (n0 + w_col[f]) % m.K) * m.stride, i0, y);
+                    eight(m.weights + (blk.row + (n0 + w_col) % m.K) * m.stride, i0 + 8 * w_group, y);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) w[f][e] += y[e];
+                    for (int e = 0; e < 8; ++e) w[e] += y[e];
                 }
         };
-        auto stage_weights = [&](int i0, int buf, int f) {
+        auto stage_weights = [&](int i0, int buf) {
             float x[8];
             uint4 pl[3];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = w[f][e] * kUp;
+            for (int e = 0; e < 8; ++e) x[e] = w[e] * kUp;
             if (i0 + 16 > n_samples)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = i0 + 8 * w_group + e < n_samples ? x[e] : 0.0f;
             split8(x, pl);
 #pragma unroll
-            for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col[f]] = pl[p];
+            for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col] = pl[p];
         };
         __syncthreads();                               // the segment before is read
         if (of_ratios) fetch_ratios(0);
-#pragma unroll
-        for (int f = 0; f < WT; ++f)
-            if (of_weights) fetch_weights(0, f);
+        if (of_weights) fetch_weights(0);
         if (of_ratios) { stage_ratios(0, 0); fetch_ratios(16); }
-#pragma unroll
-        for (int f = 0; f < WT; ++f)
-            if (of_weights) { stage_weights(0, 0, f); fetch_weights(16, f); }
+        if (of_weights) { stage_weights(0, 0); fetch_weights(16); }
         __syncthreads();
         for (int i0 = 0, buf = 0; i0 < n_samples; i0 += 16, buf ^= 1) {
             const bool next = i0 + 16 < n_samples;
-            uint4 rp[IC][3];
+            uint4 rp[I][3];
 #pragma unroll
-            for (int i = 0; i < IC; ++i)
+            for (int i = 0; i < I; ++i)
 #pragma unroll
                 for (int p = 0; p < 3; ++p) rp[i][p] = rs[buf][p][half][cw + 32 * i + col];
 #pragma unroll
-            for (int k = 0; k < IN; ++k) {
+            for (int k = 0; k < I; ++k) {
                 uint4 wp[3];
 #pragma unroll
                 for (int p = 0; p < 3; ++p) wp[p] = ws[buf][p][half][nw + 32 * k + col];
@@ -591,41 +611,41 @@ __global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_
 #pragma unroll
                     for (int p = sum; p >= 0; --p)
 #pragma unroll
-                        for (int i = 0; i < IC; ++i) acc[i][k] = mfma(rp[i][p], wp[sum - p], acc[i][k]);
-                if (next && k < WT && of_weights) { stage_weights(i0 + 16, buf ^ 1, k); fetch_weights(i0 + 32, k); }
-                if (next && k == (IN == 4 ? 2 : IN - 1) && of_ratios) { stage_ratios(i0 + 16, buf ^ 1); fetch_ratios(i0 + 32); }
+                        for (int i = 0; i < I; ++i) acc[i][k] = mfma(rp[i][p], wp[sum - p], acc[i][k]);
+                if (next && k == 0 && of_weights) { stage_weights(i0 + 16, buf ^ 1); fetch_weights(i0 + 32); }
+                if (next && k == I - 1 && of_ratios) { stage_ratios(i0 + 16, buf ^ 1); fetch_ratios(i0 + 32); }
                 __builtin_amdgcn_sched_barrier(0);
             }
             __syncthreads();
         }
     }
-    if (SCAN && none && accumulate) return;
+    if (MARKED && none && accumulate) return;
     // A whole tile of tables below 4 GiB: 32-bit offsets from addresses that all lanes share, a square's entries on their way while the one
     // before is stored.  Else entry by entry.
     auto finish = [&](auto add) {
         constexpr bool ADD = decltype(add)::value;
         float t[2][16];
-        auto offset = [&](int sq) { return (uint32_t)((o_at[nw + 32 * (sq / IC) + col] + (c0 + cw + 32 * (sq % IC) + 4 * half) * m.K) * 4); };
+        auto offset = [&](int sq) { return (uint32_t)((o_at[nw + 32 * (sq / I) + col] + (c0 + cw + 32 * (sq % I) + 4 * half) * m.K) * 4); };
         auto entry = [&](int e) { return (int64_t)(8 * (e / 4) + e % 4) * m.K * 4; };
         auto fetch = [&](int sq) {
             const uint32_t at = offset(sq);
-            if (SCAN && none) return;                  // the sums are zero
+            if (MARKED && none) return;                  // the sums are zero
 #pragma unroll
             for (int e = 0; e < 16; ++e) t[sq & 1][e] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(tables) + entry(e) + at);
         };
         fetch(0);
 #pragma unroll
-        for (int sq = 0; sq < IC * IN; ++sq) {
-            if (sq + 1 < IC * IN) fetch(sq + 1);
+        for (int sq = 0; sq < I * I; ++sq) {
+            if (sq + 1 < I * I) fetch(sq + 1);
             const uint32_t at = offset(sq);
-            if (w_at[nw + 32 * (sq / IC) + col] >= 0) {
+            if (w_at[nw + 32 * (sq / I) + col] >= 0) {
                 float old[16];
                 if (ADD)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) old[e] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(flow) + entry(e) + at);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float v = SCAN && none ? 0.0f : scale * (t[sq & 1][e] * (acc[sq % IC][sq / IC][e] * kDown));
+                    const float v = MARKED && none ? 0.0f : scale * (t[sq & 1][e] * acc[sq % I][sq / I][e]);
                     *reinterpret_cast<float *>(reinterpret_cast<char *>(flow) + entry(e) + at) = ADD ? old[e] + v : v;
                 }
             }
@@ -638,14 +658,14 @@ __global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_
         return;
     }
 #pragma unroll
-    for (int sq = 0; sq < IC * IN; ++sq) {
-        const int n = nw + 32 * (sq / IC) + col;
+    for (int sq = 0; sq < I * I; ++sq) {
+        const int n = nw + 32 * (sq / I) + col;
         if (w_at[n] < 0) continue;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int64_t c = c0 + cw + 32 * (sq % IC) + 4 * half + 8 * (e / 4) + e % 4, at = o_at[n] + c * m.K;
+            const int64_t c = c0 + cw + 32 * (sq % I) + 4 * half + 8 * (e / 4) + e % 4, at = o_at[n] + c * m.K;
             if (c < m.n_cats) {
-                const float v = scale * (tables[at] * (acc[sq % IC][sq / IC][e] * kDown));
+                const float v = scale * (tables[at] * acc[sq % I][sq / I][e]);
                 flow[at] = accumulate ? flow[at] + v : v;
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -661,7 +681,7 @@ __global__ __launch_bounds__(256, IN == 4 ? 2 : IN == 2 ? 3 : 4) void k_predict_
 // is 10^-6 of a logarithm of -4, but as much as the logarithm's own rounding allows at -10.
 static void launch_predict(const pc_mixture &m, const float *tables, int32_t B, float *logp, int64_t ld, hipStream_t s)
 {
-    const int64_t few_rows = 64 / (m.K / 4) * kFewRows;                  // categories of a wave
+    const int64_t few_rows = 64 / ((m.K + 3) / 4) * kFewRows;                  // categories of a wave
     if (B <= 2 && m.n_cats >= 512 * few_rows) {
         const dim3 grid((unsigned)((m.n_cats + 4 * few_rows - 1) / (4 * few_rows)));
         if (B == 1) hipLaunchKernelGGL((k_predict_few<1>), grid, dim3(256), 0, s, m, tables, B, logp, ld);
@@ -688,9 +708,29 @@ static void launch_predict(const pc_mixture &m, const float *tables, int32_t B, 
 #undef PC_PREDICT
 }
 
-static pc_status check_mixture(const pc_mixture *m, const float *tables, int32_t B)
+// Tiles of 64 ic categories x 64 ic columns, over all of the tables; category tiles in eights, one to an XCD.
+static int64_t flow_tiles(const pc_mixture &m, int64_t ic)
 {
-    if (!m || !tables || !m->weights) return fail(PC_ERR_ARG, "NULL argument");
+    return ((m.n_cats + 64 * ic - 1) / (64 * ic) + 7) / 8 * 8 * (((int64_t)m.n_blocks * m.K + 64 * ic - 1) / (64 * ic));
+}
+// Tiles of 128 x 128 where there are very many (4096 states x 50257: B = 32 389 us against 412 by 64 x 64, B = 256 1020 against 1420); else, where
+// they would cover the GPU in two or three rounds of workgroups, 64 x 64 (512 states: B = 16 58 us against 86, B = 96 97 against 112).
+static bool flow_wide(const pc_mixture &m) { return flow_tiles(m, 2) >= 4096; }
+
+// Scratch of the flows: k_flow_prepare's wt, then (from byte `marks` on) its marks.  Preparing pays from some 64 samples on where tiles are
+// wide (4096 states x 50257, B = 64: 64 categories a sample 376 us against 447, gradients without zeros 447 against 450), from 128 where they are not
+// (512 states, B = 128: without zeros 126 against 116; B = 256 with 64 categories a sample 81 against 176).
+struct FlowSpace { size_t marks, bytes; };
+static FlowSpace flow_space(const pc_mixture &m, int32_t B)
+{
+    if (B < (flow_wide(m) ? 64 : 128)) return {0, 0};
+    const size_t wt = ((size_t)B * m.n_blocks * m.K * 4 + 15) / 16 * 16;
+    return {wt, wt + (m.n_cats + 63ull) / 64 * ((B + 31ull) / 32) * 4};
+}
+
+static pc_status check_mixture(const pc_mixture *m, int32_t B)
+{
+    if (!m || !m->weights) return fail(PC_ERR_ARG, "NULL argument");
     if (m->K < 1 || m->K > 128) return fail(PC_ERR_ARG, "K must be in 1 .. 128");
     if (m->n_blocks < 1 || m->n_cats < 1 || m->n_tables < 1 || m->n_rows < 1)
         return fail(PC_ERR_ARG, "n_blocks, n_cats, n_tables and n_rows must be positive");
@@ -702,7 +742,6 @@ static pc_status check_mixture(const pc_mixture *m, const float *tables, int32_t
     if (m->n_cats > 1 << 29) return fail(PC_ERR_TOO_LARGE, "more than 2^29 categories");        // a grid has fewer than 2^32 threads along x
     if (!m->rows && (int64_t)m->n_blocks * m->K > m->n_rows) return fail(PC_ERR_ARG, "weights have fewer than n_blocks * K rows");
     if (!m->table && m->n_blocks > m->n_tables) return fail(PC_ERR_ARG, "fewer tables than blocks");
-    if (!aligned_to(tables, 16)) return fail(PC_ERR_ARG, "tables must be 16-byte aligned");
     if (!aligned_to(m->weights, 4) || !aligned_to(m->rows, 4) || !aligned_to(m->table, 4))
         return fail(PC_ERR_ARG, "weights, rows and table must be 4-byte aligned");
     return PC_OK;
@@ -716,12 +755,13 @@ extern "C" {
 
 pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *stream)
 {
-    const pc_status st = check_mixture(m, tables, B);
+    const pc_status st = check_mixture(m, B);
     if (st != PC_OK) return st;
-    if (!logp) return fail(PC_ERR_ARG, "NULL argument");
+    if (!tables || !logp) return fail(PC_ERR_ARG, "NULL argument");
+    if (!aligned_to(tables, 16)) return fail(PC_ERR_ARG, "tables must be 16-byte aligned");
     if (ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4)) return fail(PC_ERR_ARG, "logp must be 4-byte aligned");
-    if (m->K % 4 == 0) {
+    if (m->K >= 4) {
         launch_predict(*m, tables, B, logp, ld, (hipStream_t)stream);
         return launched();
     }
@@ -730,12 +770,23 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
     return launched();
 }
 
-pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t B, const float *logp, int64_t logp_ld,
-                              const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow, void *stream)
+pc_status pc_predict_backward_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes)
 {
-    const pc_status st = check_mixture(m, tables, B);
+    const pc_status st = check_mixture(m, B);
     if (st != PC_OK) return st;
-    if (!logp || !dlogp || !table_flow) return fail(PC_ERR_ARG, "NULL argument");
+    if (!bytes) return fail(PC_ERR_ARG, "NULL argument");
+    *bytes = flow_space(*m, B).bytes;
+    return PC_OK;
+}
+
+pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t B, const float *logp, int64_t logp_ld,
+                              const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow, void *workspace,
+                              size_t workspace_bytes, void *stream)
+{
+    const pc_status st = check_mixture(m, B);
+    if (st != PC_OK) return st;
+    if (!tables || !logp || !dlogp || !table_flow) return fail(PC_ERR_ARG, "NULL argument");
+    if (!aligned_to(tables, 16)) return fail(PC_ERR_ARG, "tables must be 16-byte aligned");
     if (logp_ld < m->n_cats || dlogp_ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4) || !aligned_to(dlogp, 4)) return fail(PC_ERR_ARG, "logp and dlogp must be 4-byte aligned");
     if (!aligned_to(table_flow, 16)) return fail(PC_ERR_ARG, "table_flow must be 16-byte aligned");
@@ -743,19 +794,28 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     // 981; by 64 x 64 412 at B = 32); of fewer, which such tiles would cover in two or three rounds of workgroups, 64 x 64 (512 states: B = 16
     // 58 us against 86, B = 96 97 against 112).  Looking for samples to leave out pays from some 128 on.
     const int64_t H = (int64_t)m->n_blocks * m->K;
-    const auto tiles = [&](int64_t tc, int64_t tn) { return ((m->n_cats + tc - 1) / tc + 7) / 8 * 8 * ((H + tn - 1) / tn); };
     const hipStream_t s = (hipStream_t)stream;
-    if (tiles(64, 64) > 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of flows");
-#define PC_FLOW(IC, IN, SCAN)                                                                                                              \
-    hipLaunchKernelGGL((m->table ? k_predict_flow<IC, IN, SCAN, true> : k_predict_flow<IC, IN, SCAN, false>), dim3((unsigned)tiles(64 * IC, 64 * IN)), dim3(256), 0, \
-                       s, *m, tables, B, logp, logp_ld, dlogp, dlogp_ld, scale, accumulate, table_flow)
-    if (tiles(128, 128) >= 4096) {
-        if (B >= 128) PC_FLOW(2, 4, true);
-        else PC_FLOW(2, 2, false);
-    } else {
-        if (B >= 128) PC_FLOW(1, 1, true);
-        else PC_FLOW(1, 1, false);
+    if (flow_tiles(*m, 1) > 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of flows");
+    const FlowSpace f = flow_space(*m, B);
+    if (workspace_bytes < f.bytes) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_backward_workspace_bytes");
+    if (f.bytes && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
+    float *wt = (float *)workspace;
+    uint32_t *marks = (uint32_t *)((char *)workspace + f.marks);
+    if (f.bytes) {
+        const int64_t turns = (H + 63) / 64 * ((B + 63ll) / 64), jobs = (m->n_cats + 63ll) / 64 * ((B + 31ll) / 32);
+        if (turns + jobs / 4 >= 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of weights and gradients");
+        hipLaunchKernelGGL(k_flow_prepare, dim3((unsigned)(turns + (jobs + 3) / 4)), dim3(256), 0, s, *m, B, dlogp, dlogp_ld, (int32_t)turns, wt, marks);
     }
+#define PC_FLOW(I, MARKED, LISTS)                                                                                                       \
+    hipLaunchKernelGGL((k_predict_flow<I, MARKED, LISTS>), dim3((unsigned)flow_tiles(*m, I)), dim3(256), 0, s, *m, tables, B, logp, logp_ld, \
+                       dlogp, dlogp_ld, scale, accumulate, table_flow, wt, marks)
+    const bool wide = flow_wide(*m);
+    if (f.bytes && wide) PC_FLOW(2, true, false);
+    else if (f.bytes) PC_FLOW(1, true, false);
+    else if (m->table && wide) PC_FLOW(2, false, true);
+    else if (m->table) PC_FLOW(1, false, true);
+    else if (wide) PC_FLOW(2, false, false);
+    else PC_FLOW(1, false, false);
 #undef PC_FLOW
     return launched();
 }

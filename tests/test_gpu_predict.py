@@ -67,7 +67,9 @@ SIZES = [(1, 1, 1, 1), (1, 3, 2, 5), (2, 1, 7, 33), (7, 5, 65, 31), (16, 1, 64, 
          (127, 1, 127, 127), (128, 3, 517, 40), (128, 2, 5003, 1), (128, 1, 32, 513), (64, 1, 4099, 300),
          # every tile shape of the rules: 64, 128 and 256 samples a wave, two planes and three, blocks shorter and longer than a chunk; flows by 128 x 128
          (16, 4, 33000, 40), (20, 3, 32800, 100), (32, 4, 17000, 300), (48, 2, 33000, 65), (128, 1, 4000, 600), (20, 5, 4000, 1200), (100, 1, 3000, 1300),
-         (128, 16, 33000, 37), (64, 8, 16411, 2), (128, 16, 32901, 1), (33, 8, 17000, 70)]
+         (128, 16, 33000, 37), (64, 8, 16411, 2), (128, 16, 32901, 1), (33, 8, 17000, 70),
+         # blocks that are no multiple of four states: each remainder, few samples and many, the shortest blocks of the matrix cores
+         (4, 9, 100, 40), (5, 7, 33000, 1), (6, 300, 60, 200), (7, 600, 5000, 33), (9, 5, 33000, 2), (127, 3, 8200, 300), (33, 69, 582, 460), (3, 40, 90, 70)]
 
 
 @pytest.mark.parametrize("K,nb,V,B", SIZES)
@@ -123,7 +125,7 @@ def test_block_lists_with_gaps_shared_tables_and_entries_out_of_range():
         check_flow(got[j], (ws @ r).T * t[j], (ws @ np.abs(r)).T * t[j], B * len(mine))
 
 
-@pytest.mark.parametrize("B,density", [(128, 0.0), (130, 0.002), (300, 0.01), (700, 0.002), (1100, 0.02), (256, 0.9)])
+@pytest.mark.parametrize("B,density", [(64, 0.004), (127, 0.02), (128, 0.0), (130, 0.002), (300, 0.01), (700, 0.002), (1100, 0.02), (256, 0.9)])
 @pytest.mark.parametrize("shared", [False, True])
 @pytest.mark.parametrize("V", [16500, 1001])
 def test_flows_of_targets_of_few_categories(B, density, shared, V):

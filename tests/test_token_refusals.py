@@ -30,7 +30,7 @@ MIXTURE = [(dict(K=0), "PC_ERR_ARG"), (dict(K=129), "PC_ERR_ARG"), (dict(n_block
 def test_predict_refuses_mixtures(change, want):
     m = mixture(**change)
     assert status(pcb.lib().pc_predict(C.byref(m), P, 16, P, 10, None)) == want
-    assert status(pcb.lib().pc_predict_backward(C.byref(m), P, 16, P, 10, P, 10, 1.0, 1, P, None)) == want
+    assert status(pcb.lib().pc_predict_backward(C.byref(m), P, 16, P, 10, P, 10, 1.0, 1, P, P, 1 << 30, None)) == want
 
 
 @pytest.mark.parametrize("args,want", [((None, 16, P, 10), "PC_ERR_ARG"), ((P + 4, 16, P, 10), "PC_ERR_ARG"), ((P, 0, P, 10), "PC_ERR_ARG"), ((P, -1, P, 10), "PC_ERR_ARG"),
@@ -46,7 +46,18 @@ def test_predict_refuses_arguments(args, want):
                                   (P + 2, 10, P, 10, 1.0, 1, P)])
 def test_predict_backward_refuses_arguments(args):
     m = mixture()
-    assert status(pcb.lib().pc_predict_backward(C.byref(m), P, 16, *args, None)) == "PC_ERR_ARG"
+    assert status(pcb.lib().pc_predict_backward(C.byref(m), P, 16, *args, P, 1 << 30, None)) == "PC_ERR_ARG"
+
+
+def test_predict_backward_refuses_workspaces():
+    m, n, L = mixture(stride=300), C.c_size_t(), pcb.lib()
+    assert status(L.pc_predict_backward_workspace_bytes(C.byref(m), 16, C.byref(n))) == "PC_OK" and n.value == 0
+    assert status(L.pc_predict_backward_workspace_bytes(C.byref(m), 300, C.byref(n))) == "PC_OK" and n.value >= 300 * 128 * 4 + 10 * 4
+    for ws, size, want in ((P, n.value - 1, "PC_ERR_WORKSPACE"), (None, 0, "PC_ERR_WORKSPACE"), (None, n.value, "PC_ERR_ARG"), (P + 8, n.value, "PC_ERR_ARG")):
+        assert status(L.pc_predict_backward(C.byref(m), P, 300, P, 10, P, 10, 1.0, 1, P, ws, size, None)) == want
+    assert status(L.pc_predict_backward_workspace_bytes(None, 16, C.byref(n))) == "PC_ERR_ARG"
+    assert status(L.pc_predict_backward_workspace_bytes(C.byref(m), 16, None)) == "PC_ERR_ARG"
+    assert status(L.pc_predict_backward_workspace_bytes(C.byref(m), 301, C.byref(n))) == "PC_ERR_ARG"
 
 
 def test_mixtures_of_circuits_need_a_device_and_a_variable():
