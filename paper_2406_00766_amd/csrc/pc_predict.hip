@@ -467,7 +467,7 @@ constexpr int kSegment = 512;
 template <int I, bool MARKED, bool LISTS>
 __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_mixture m, const float *__restrict__ tables, int32_t B, const float *__restrict__ logp,
                                                          int64_t lp_ld, const float *__restrict__ dlogp, int64_t dl_ld, float scale, int32_t accumulate,
-                                                         float *__restrict__ flow, const float *__restrict__ wt, const uint32_t *__restrict__ marks)
+                                                         float *__restrict__ flow, const float *__restrict__ wt, const uint32_t *__restrict__ marks, int32_t part, float *__restrict__ sums)
 {
     constexpr int TH = 256, TC = 64 * I, TN = 64 * I, NP = TN + 4;   // four more: the two groups of a column lie in other banks
     __shared__ uint4 rs[2][3][2][TC], ws[2][3][2][NP];                            // [buffer][plane][8 samples][category or column]
@@ -502,8 +502,9 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.0f;
     bool none = true;                                  // no sample counts for this tile
-    for (int s0 = 0; s0 < B; s0 += MARKED ? kSegment : B) {
-        const int here = MARKED ? min(kSegment, B - s0) : B;
+    const int first = MARKED ? blockIdx.y * part : 0, last = MARKED ? min(B, first + part) : B;
+    for (int s0 = first; s0 < last; s0 += MARKED ? kSegment : B) {
+        const int here = MARKED ? min(kSegment, last - s0) : B;
         bool all = true;
         if (MARKED) {                                  // the samples that count, in order
             __syncthreads();
@@ -619,6 +620,14 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
             __syncthreads();
         }
     }
+    if (MARKED && I == 1 && sums) {                    // a part of the samples
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int64_t c = c0 + cw + 4 * half + 8 * (e / 4) + e % 4;
+            if (c < m.n_cats && n0 + nw + col < H) sums[(blockIdx.y * (int64_t)m.n_cats + c) * H + n0 + nw + col] = acc[0][0][e];
+        }
+        return;
+    }
     if (MARKED && none && accumulate) return;
     // A whole tile of tables below 4 GiB: 32-bit offsets from addresses that all lanes share, a square's entries on their way while the one
     // before is stored.  Else entry by entry.
@@ -673,6 +682,27 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
     }
 }
 
+// The flows from the sums of `parts` parts of the samples: 64 columns x 16 categories a workgroup.
+__global__ __launch_bounds__(256) void k_flow_join(const pc_mixture m, const float *__restrict__ tables, const float *__restrict__ sums, int32_t parts, float scale,
+                                                   int32_t accumulate, float *__restrict__ flow)
+{
+    __shared__ int64_t w_at[64], o_at[64];
+    __shared__ int32_t more[64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, H = m.n_blocks * m.K, n = blockIdx.x * 64 + lane;
+    if (wave == 0) flow_column(m, n, w_at[lane], o_at[lane], more[lane]);
+    __syncthreads();
+    if (w_at[lane] < 0) return;
+    for (int i = 0; i < 4; ++i) {
+        const int64_t c = blockIdx.y * 16ll + wave + 4 * i, at = o_at[lane] + c * m.K;
+        if (c >= m.n_cats) return;
+        float sum = 0.0f;
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) sum += sums[(p * (int64_t)m.n_cats + c) * H + n];
+        const float v = scale * (tables[at] * sum);
+        flow[at] = accumulate ? flow[at] + v : v;
+    }
+}
+
 // One or two samples of many categories: no matrix cores (4096 states x 50257 at one sample: 171 us against 211 with them, at four 212 against 200),
 // where that makes waves enough for two to a CU.
 // Samples a wave: as many of 256 as there are, so that the tables are read once; fewer where that leaves a SIMD without a wave (the
@@ -717,15 +747,21 @@ static int64_t flow_tiles(const pc_mixture &m, int64_t ic)
 // they would cover the GPU in two or three rounds of workgroups, 64 x 64 (512 states: B = 16 58 us against 86, B = 96 97 against 112).
 static bool flow_wide(const pc_mixture &m) { return flow_tiles(m, 2) >= 4096; }
 
-// Scratch of the flows: k_flow_prepare's wt, then (from byte `marks` on) its marks.  Preparing pays from some 64 samples on where tiles are
+// Scratch of the flows: k_flow_prepare's wt, then (from byte `marks` on) its marks, then (from byte `sums` on) the sums of parts.  Preparing pays from some 64 samples on where tiles are
 // wide (4096 states x 50257, B = 64: 64 categories a sample 376 us against 447, gradients without zeros 447 against 450), from 128 where they are not
 // (512 states, B = 128: without zeros 126 against 116; B = 256 with 64 categories a sample 81 against 176).
-struct FlowSpace { size_t marks, bytes; };
+// Where 64 x 64 tiles are few the samples are dealt out to several workgroups a tile, `part` each (a multiple of 64), whose sums k_flow_join
+// adds up, always in the same order (128 states x 256, B = 512 28 us against 53; 512 states x 4000, B = 256 in 1000 workgroups 39 against 30).
+constexpr int64_t kFlowGroups = 512, kFlowParts = 64;
+struct FlowSpace { size_t marks, sums, bytes; int32_t part, parts; };
 static FlowSpace flow_space(const pc_mixture &m, int32_t B)
 {
-    if (B < (flow_wide(m) ? 64 : 128)) return {0, 0};
-    const size_t wt = ((size_t)B * m.n_blocks * m.K * 4 + 15) / 16 * 16;
-    return {wt, wt + (m.n_cats + 63ull) / 64 * ((B + 31ull) / 32) * 4};
+    if (B < (flow_wide(m) ? 64 : 128)) return {0, 0, 0, B, 1};
+    const int64_t H = (int64_t)m.n_blocks * m.K, tiles = (m.n_cats + 63ll) / 64 * ((H + 63) / 64);
+    const int64_t want = std::max<int64_t>(1, std::min(kFlowGroups / tiles, kFlowParts));
+    const int32_t part = (int32_t)(((B + want - 1) / want + 63) / 64 * 64), parts = (B + part - 1) / part;
+    const size_t marks = ((size_t)B * H * 4 + 15) / 16 * 16, sums = marks + ((size_t)((m.n_cats + 63ll) / 64 * ((B + 31ll) / 32)) * 4 + 15) / 16 * 16;
+    return {marks, sums, sums + (parts > 1 ? (size_t)parts * m.n_cats * H * 4 : 0), part, parts};
 }
 
 static pc_status check_mixture(const pc_mixture *m, int32_t B)
@@ -801,14 +837,15 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     if (f.bytes && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
     float *wt = (float *)workspace;
     uint32_t *marks = (uint32_t *)((char *)workspace + f.marks);
+    float *sums = f.parts > 1 ? (float *)((char *)workspace + f.sums) : nullptr;
     if (f.bytes) {
         const int64_t turns = (H + 63) / 64 * ((B + 63ll) / 64), jobs = (m->n_cats + 63ll) / 64 * ((B + 31ll) / 32);
         if (turns + jobs / 4 >= 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of weights and gradients");
         hipLaunchKernelGGL(k_flow_prepare, dim3((unsigned)(turns + (jobs + 3) / 4)), dim3(256), 0, s, *m, B, dlogp, dlogp_ld, (int32_t)turns, wt, marks);
     }
 #define PC_FLOW(I, MARKED, LISTS)                                                                                                       \
-    hipLaunchKernelGGL((k_predict_flow<I, MARKED, LISTS>), dim3((unsigned)flow_tiles(*m, I)), dim3(256), 0, s, *m, tables, B, logp, logp_ld, \
-                       dlogp, dlogp_ld, scale, accumulate, table_flow, wt, marks)
+    hipLaunchKernelGGL((k_predict_flow<I, MARKED, LISTS>), dim3((unsigned)flow_tiles(*m, I), f.parts), dim3(256), 0, s, *m, tables, B, logp, logp_ld, \
+                       dlogp, dlogp_ld, scale, accumulate, table_flow, wt, marks, f.part, sums)
     const bool wide = flow_wide(*m);
     if (f.bytes && wide) PC_FLOW(2, true, false);
     else if (f.bytes) PC_FLOW(1, true, false);
@@ -817,6 +854,8 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     else if (wide) PC_FLOW(2, false, false);
     else PC_FLOW(1, false, false);
 #undef PC_FLOW
+    if (sums)
+        hipLaunchKernelGGL(k_flow_join, dim3((unsigned)((H + 63) / 64), (unsigned)((m->n_cats + 15ll) / 16)), dim3(256), 0, s, *m, tables, sums, f.parts, scale, accumulate, table_flow);
     return launched();
 }
 
