@@ -264,7 +264,9 @@ pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void
 /* Predictive distribution:  logp[b][c] = log sum_j sum_k weights[rows[j] + k][b] * tables[table[j]][c][k],  b < B, c < n_cats,
  * ld >= n_cats floats between the rows of logp.  A probability below FLT_MIN (a sample without weights: all of them) gives
  * -inf. */
-pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *stream);
+pc_status pc_predict_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
+pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace,
+                     size_t workspace_bytes, void *stream);
 
 /* Its flows for a gradient dlogp of an objective with respect to logp, the weights held fixed (the responsibilities of an
  * EM step):

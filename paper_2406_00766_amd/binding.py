@@ -89,7 +89,7 @@ EXPORTS = ["pc_compile", "pc_compile_host", "pc_destroy", "pc_last_error", "pc_g
            "pc_forward_static", "pc_backward", "pc_em_step", "pc_profile_enable", "pc_profile_read", "pc_kernel_class_name",
            "pc_measure_copy", "pc_measure_mfma_f32", "pc_collapse", "pc_collapsed_dag", "pc_collapsed_theta",
            "pc_collapsed_block_map", "pc_collapsed_destroy", "pc_order_for_scratch", "pc_set_wait_limit",
-           "pc_get_mixture", "pc_predict", "pc_predict_backward_workspace_bytes", "pc_predict_backward",
+           "pc_get_mixture", "pc_predict_workspace_bytes", "pc_predict", "pc_predict_backward_workspace_bytes", "pc_predict_backward",
            "pc_distill_workspace_bytes", "pc_distill_forward", "pc_distill_backward", "pc_beam_workspace_bytes",
            "pc_beam_select", "pc_beam_reorder"]
 
@@ -142,7 +142,8 @@ def lib():
         L.pc_collapsed_destroy.argtypes = [C.c_void_p]
         L.pc_collapsed_destroy.restype = None
         L.pc_get_mixture.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(pc_mixture)]
-        L.pc_predict.argtypes = [C.POINTER(pc_mixture), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+        L.pc_predict_workspace_bytes.argtypes = [C.POINTER(pc_mixture), C.c_int32, C.POINTER(C.c_size_t)]
+        L.pc_predict.argtypes = [C.POINTER(pc_mixture), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
         L.pc_predict_backward.argtypes = [C.POINTER(pc_mixture), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                           C.c_float, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.pc_predict_backward_workspace_bytes.argtypes = [C.POINTER(pc_mixture), C.c_int32, C.POINTER(C.c_size_t)]
@@ -479,26 +480,50 @@ def _rows(name, t, dtype, shape, index):
     return t.data_ptr(), _ld(t)
 
 
-def pc_predict(m: mixture, tables, B, logp, stream=None):
-    """logp float32 [B, n_cats] (rows may be strided) = log sum of weights * tables."""
+def _bytes_of(function, struct, *args):
+    n = C.c_size_t()
+    _check(function(C.byref(struct), *args, C.byref(n)))
+    return n.value
+
+
+def _scratch(workspace, size, index, stream):
+    """(address, bytes) of the caller's workspace, and what keeps it; None: `size` bytes are allocated on the call's stream, so that,
+    freed, they serve that stream's later work only."""
+    if workspace is not None or not size:
+        return _workspace(workspace, index), workspace
+    import torch
+    if stream is None:
+        t = torch.empty(size, dtype=torch.uint8, device=index)
+    else:
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=index) if isinstance(stream, int) else stream):
+            t = torch.empty(size, dtype=torch.uint8, device=index)
+    return (t.data_ptr(), size), t
+
+
+def pc_predict_workspace_bytes(m: mixture, B) -> int:
+    return int(_bytes_of(lib().pc_predict_workspace_bytes, m.struct, int(B)))
+
+
+def pc_predict(m: mixture, tables, B, logp, stream=None, workspace=None):
+    """logp float32 [B, n_cats] (rows may be strided) = log sum of weights * tables.  workspace: a uint8 tensor of
+    pc_predict_workspace_bytes; None: one is allocated where the call needs it."""
     import torch
     s, B = m.struct, int(B)
     _floats("tables", tables, s.n_tables * s.n_cats * s.K, m.index)
     if B > m.columns:
         _refuse("weights have fewer than B columns")
     out = _rows("logp", logp, torch.float32, (B, s.n_cats), m.index)
-    _call(m.index, stream, lib().pc_predict, C.byref(s), tables.data_ptr(), B, *out)
+    (ws, size), keep = _scratch(workspace, workspace is None and _bytes_of(lib().pc_predict_workspace_bytes, s, B), m.index, stream)
+    _call(m.index, stream, lib().pc_predict, C.byref(s), tables.data_ptr(), B, *out, ws, size)
 
 
 def pc_predict_backward_workspace_bytes(m: mixture, B) -> int:
-    n = C.c_size_t()
-    _check(lib().pc_predict_backward_workspace_bytes(C.byref(m.struct), int(B), C.byref(n)))
-    return int(n.value)
+    return int(_bytes_of(lib().pc_predict_backward_workspace_bytes, m.struct, int(B)))
 
 
 def pc_predict_backward(m: mixture, tables, B, logp, dlogp, scale, table_flow, accumulate=True, stream=None, workspace=None):
     """Table flows for a gradient dlogp [B, n_cats] of an objective; added to table_flow, or stored.  workspace: a uint8 tensor of
-    pc_predict_backward_workspace_bytes; None: one is allocated on the call's stream."""
+    pc_predict_backward_workspace_bytes; None: one is allocated where the call needs it."""
     import torch
     s, B = m.struct, int(B)
     n = s.n_tables * s.n_cats * s.K
@@ -508,16 +533,9 @@ def pc_predict_backward(m: mixture, tables, B, logp, dlogp, scale, table_flow, a
         _refuse("weights have fewer than B columns")
     shape = (B, s.n_cats)
     args = (*_rows("logp", logp, torch.float32, shape, m.index), *_rows("dlogp", dlogp, torch.float32, shape, m.index))
-    if workspace is None:
-        size = pc_predict_backward_workspace_bytes(m, B)
-        if size:
-            if stream is None:
-                workspace = torch.empty(size, dtype=torch.uint8, device=m.index)
-            else:                                       # memory of the stream that uses it: freed, it serves that stream's later work only
-                with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=m.index) if isinstance(stream, int) else stream):
-                    workspace = torch.empty(size, dtype=torch.uint8, device=m.index)
+    (ws, size), keep = _scratch(workspace, workspace is None and _bytes_of(lib().pc_predict_backward_workspace_bytes, s, B), m.index, stream)
     _call(m.index, stream, lib().pc_predict_backward, C.byref(s), tables.data_ptr(), B, *args, float(scale), 1 if accumulate else 0,
-          table_flow.data_ptr(), *_workspace(workspace, m.index))
+          table_flow.data_ptr(), ws, size)
 
 
 class distill:

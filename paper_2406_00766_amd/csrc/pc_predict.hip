@@ -23,6 +23,7 @@ __device__ inline MixBlock mix_block(const pc_mixture &m, int j)
 }
 
 constexpr float kLogFltMin = -87.33654475f;           // log FLT_MIN
+__device__ inline float log_p(float p) { return p < __FLT_MIN__ ? PC_NEG_INF_F : logf(p); }
 
 // K below 4.  64 categories x 64 samples a workgroup, 4 x 4 sums a thread, the states in steps of 16 through LDS.
 __global__ __launch_bounds__(256) void k_predict_any(const pc_mixture m, const float *__restrict__ tables, int32_t B,
@@ -55,10 +56,7 @@ __global__ __launch_bounds__(256) void k_predict_any(const pc_mixture m, const f
     }
     for (int i = 0; i < 4; ++i)
         for (int j = 0; j < 4; ++j)
-            if (b0 + tb + i < B && c0 + tc + j < m.n_cats) {
-                const float p = acc[i][j];
-                logp[(int64_t)(b0 + tb + i) * ld + c0 + tc + j] = p < __FLT_MIN__ ? PC_NEG_INF_F : logf(p);
-            }
+            if (b0 + tb + i < B && c0 + tc + j < m.n_cats) logp[(int64_t)(b0 + tb + i) * ld + c0 + tc + j] = log_p(acc[i][j]);
 }
 
 // ---- matrix-core kernels: K of at least 4 ----
@@ -114,13 +112,13 @@ __device__ inline floatx16 mfma(const uint4 &a, const uint4 &b, const floatx16 &
 constexpr int kWindow = 2048;
 template <int NT, int WAVES, int SPLIT, int KC, int PLANES, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 3 : 4) void k_predict(const pc_mixture m, const float *__restrict__ tables, int32_t B,
-                                                                        float *__restrict__ logp, int64_t ld)
+                                                                        float *__restrict__ logp, int64_t ld, int32_t len, float *__restrict__ sums)
 {
     constexpr int TH = 64 * WAVES, NB = 32 * NT, STEPS = KC / 16, KW = KC * SPLIT, TASKS = NB * KW / 8, FT = (TASKS + TH - 1) / TH;
     __shared__ uint4 planes[2][PLANES][KW / 8][NB];   // [buffer][plane][8 states][sample]
     __shared__ int64_t t_at[kWindow / 4], w_at[kWindow / 4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5, part = wave % SPLIT;
-    const int Kg = group_states(m.K), H = m.n_blocks * Kg, c0 = (blockIdx.x * (WAVES / SPLIT) + wave / SPLIT) * 32, b0 = blockIdx.y * NB;
+    const int Kg = group_states(m.K), first = blockIdx.z * len, H = min(m.n_blocks * Kg - first, len), c0 = (blockIdx.x * (WAVES / SPLIT) + wave / SPLIT) * 32, b0 = blockIdx.y * NB;
     const int64_t mine = (int64_t)min(c0 + col, m.n_cats - 1) * m.K;     // a category behind the last reads that one's row again
     const int here = min(NB, B - b0);                  // samples of this workgroup
     floatx16 acc[NT];
@@ -142,8 +140,8 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
 
     auto fill_window = [&](int n0) {
         for (int i = threadIdx.x; i < kWindow / 4; i += TH) {
-            const int n = n0 + 4 * i;
-            const MixBlock blk = n < H ? mix_block(m, n / Kg) : MixBlock{-1, -1};
+            const int n = first + n0 + 4 * i;
+            const MixBlock blk = n0 + 4 * i < H ? mix_block(m, n / Kg) : MixBlock{-1, -1};
             const int k = group_start(m.K, n % Kg);
             t_at[i] = blk.row >= 0 ? (int64_t)blk.table * m.n_cats * m.K + k : -1;
             w_at[i] = blk.row >= 0 ? (blk.row + k) * m.stride * 4 + (n % Kg - k) : -1;      // and how many to skip
@@ -155,7 +153,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     float w_raw[FT][8];
     uint32_t t_mask[WHOLE ? 1 : STEPS][2];
     int w_skip[FT][2];                                 // 4: all
-    auto fetch_weights = [&](int n0, int f) {          // of the chunk that begins with state n0
+    auto fetch_weights = [&](int n0, int f) {          // of the chunk that begins with state `first` + n0
         const int g0 = n0 % kWindow / 4;
         if (!wave_stages[f]) return;
         const int b = min(task_b[f], here - 1);
@@ -297,8 +295,22 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
         for (int e = 0; e < 16; ++e) {
             const int b = b0 + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
             const float p = acc[t][e] * (kDown * kDown);
-            if (b < B) logp[(int64_t)b * ld + c0 + col] = p < __FLT_MIN__ ? PC_NEG_INF_F : logf(p);
+            if (b < B) {
+                if (sums) sums[(blockIdx.z * (int64_t)B + b) * m.n_cats + c0 + col] = p;
+                else logp[(int64_t)b * ld + c0 + col] = log_p(p);
+            }
         }
+}
+
+// Log-probabilities from the sums over `parts` parts of the states.
+__global__ __launch_bounds__(256) void k_predict_join(const float *__restrict__ sums, int32_t parts, int32_t n_cats, int32_t B, float *__restrict__ logp, int64_t ld)
+{
+    const int64_t i = blockIdx.x * 256ll + threadIdx.x, n = (int64_t)B * n_cats;
+    if (i >= n) return;
+    float p = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < parts; ++s) p += sums[s * n + i];
+    logp[i / n_cats * ld + i % n_cats] = log_p(p);
 }
 
 // A few samples: bound by reading the tables once.  The lanes of a wave cover whole table rows (K / 4 lanes each with four states) of the
@@ -375,7 +387,7 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
                 const float o = __shfl_down(v, d);
                 if (piece + d < P && piece % (2 * d) == 0) v += o;
             }
-            if (piece == 0 && !idle && s < B && c < m.n_cats) logp[s * ld + c] = v < __FLT_MIN__ ? PC_NEG_INF_F : logf(v);
+            if (piece == 0 && !idle && s < B && c < m.n_cats) logp[s * ld + c] = log_p(v);
         }
     }
 }
@@ -703,30 +715,53 @@ __global__ __launch_bounds__(256) void k_flow_join(const pc_mixture m, const flo
     }
 }
 
-// One or two samples of many categories: no matrix cores (4096 states x 50257 at one sample: 171 us against 211 with them, at four 212 against 200),
-// where that makes waves enough for two to a CU.
-// Samples a wave: as many of 256 as there are, so that the tables are read once; fewer where that leaves a SIMD without a wave (the
-// tables of few categories stay in the caches).
+static int64_t few_rows(const pc_mixture &m) { return 64 / ((m.K + 3) / 4) * kFewRows; }      // categories of a wave of k_predict_few
+
+// How a prediction is launched.
+// One or two samples of many categories: no matrix cores (4096 states x 50257 at one sample: 168 us against 211 with them, at four 163 with them
+// against 200), where that makes waves enough for two to a CU.
 // Two planes an operand where log-probabilities are large (many categories), three where they are not: an error of 2^-18 of a probability
 // is 10^-6 of a logarithm of -4, but as much as the logarithm's own rounding allows at -10.
-static void launch_predict(const pc_mixture &m, const float *tables, int32_t B, float *logp, int64_t ld, hipStream_t s)
+// Samples a wave: as many of 256 as there are, so that the tables are read once; fewer where that leaves a SIMD without a wave (the
+// tables of few categories stay in the caches).
+// Where there is less than a workgroup to a CU and the states are many (1024: an exchange and a second launch take some 4 us) they are dealt out
+// in parts of at least 256, as many as fill the GPU once, whose sums k_predict_join adds up (4096 states x 256, B = 256 22 us against 61;
+// x 5000 63 against 144; x 16000, 2048 states, B = 500 124 against 135; with more workgroups, 1024 states x 50257, B = 64 66 against 49).
+struct PredictPlan { bool few, exact; int32_t nt, len, parts; size_t bytes; };
+static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
 {
-    const int64_t few_rows = 64 / ((m.K + 3) / 4) * kFewRows;                  // categories of a wave
-    if (B <= 2 && m.n_cats >= 512 * few_rows) {
-        const dim3 grid((unsigned)((m.n_cats + 4 * few_rows - 1) / (4 * few_rows)));
+    PredictPlan p{};
+    if (m.K < 4) return p;
+    p.few = B <= 2 && m.n_cats >= 512 * few_rows(m);
+    if (p.few) return p;
+    const int64_t rows = (m.n_cats + 31ll) / 32, H = (int64_t)m.n_blocks * ((m.K + 3) / 4 * 4), most = H < 1024 ? 1 : H / 256;
+    p.exact = m.n_cats < 4096;
+    p.nt = B > 128 && !p.exact ? 8 : B > 64 ? 4 : B > 32 ? 2 : 1;
+    const auto columns = [&] { return (B + 32ll * p.nt - 1) / (32 * p.nt); };
+    while (p.nt > 1 && rows * columns() * most < 1024) p.nt /= 2;
+    const int64_t groups = (p.nt == 8 ? (rows + 7) / 8 : p.nt > 1 ? (rows + 3) / 4 : rows) * columns();
+    const int64_t slots = 256 * (p.nt == 8 ? 1 : p.nt == 4 ? (p.exact ? 2 : 3) : p.nt == 2 ? (p.exact ? 3 : 4) : (p.exact ? 2 : 4));
+    const int64_t want = groups < 256 ? std::min(slots / groups, most) : 1;
+    p.len = (int32_t)((H + want * 128 - 1) / (want * 128) * 128);
+    p.parts = (int32_t)((H + p.len - 1) / p.len);
+    p.bytes = p.parts > 1 ? (size_t)p.parts * B * m.n_cats * 4 : 0;
+    return p;
+}
+
+static void launch_predict(const pc_mixture &m, const PredictPlan &p, const float *tables, int32_t B, float *logp, int64_t ld, float *sums, hipStream_t s)
+{
+    if (p.few) {
+        const dim3 grid((unsigned)((m.n_cats + 4 * few_rows(m) - 1) / (4 * few_rows(m))));
         if (B == 1) hipLaunchKernelGGL((k_predict_few<1>), grid, dim3(256), 0, s, m, tables, B, logp, ld);
         else hipLaunchKernelGGL((k_predict_few<2>), grid, dim3(256), 0, s, m, tables, B, logp, ld);
         return;
     }
     const int64_t rows = (m.n_cats + 31ll) / 32;
-    const bool exact = m.n_cats < 4096;
-    int nt = B > 128 && !exact ? 8 : B > 64 ? 4 : B > 32 ? 2 : 1;
-    while (nt > 1 && rows * ((B + 32 * nt - 1) / (32 * nt)) < 1024) nt /= 2;
 #define PC_PREDICT(NT, WAVES, SPLIT, KC, PLANES)                                                                               \
-    if (nt == NT && exact == (PLANES == 3)) {                                                                                  \
-        const dim3 grid((unsigned)((rows + WAVES / SPLIT - 1) / (WAVES / SPLIT)), (unsigned)((B + 32 * NT - 1) / (32 * NT)));  \
-        if (m.K % KC == 0) hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, true>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld); \
-        else hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, false>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld); \
+    if (p.nt == NT && p.exact == (PLANES == 3)) {                                                                              \
+        const dim3 grid((unsigned)((rows + WAVES / SPLIT - 1) / (WAVES / SPLIT)), (unsigned)((B + 32 * NT - 1) / (32 * NT)), p.parts);  \
+        if (m.K % KC == 0) hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, true>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums); \
+        else hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, false>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums); \
     }
     PC_PREDICT(8, 8, 1, 32, 2)
     PC_PREDICT(4, 4, 1, 32, 2)
@@ -736,6 +771,10 @@ static void launch_predict(const pc_mixture &m, const float *tables, int32_t B, 
     PC_PREDICT(2, 4, 1, 32, 3)
     PC_PREDICT(1, 4, 4, 32, 3)
 #undef PC_PREDICT
+    if (sums) {
+        const int64_t n = (int64_t)B * m.n_cats;
+        hipLaunchKernelGGL(k_predict_join, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, sums, p.parts, m.n_cats, B, logp, ld);
+    }
 }
 
 // Tiles of 64 ic categories x 64 ic columns, over all of the tables; category tiles in eights, one to an XCD.
@@ -743,9 +782,10 @@ static int64_t flow_tiles(const pc_mixture &m, int64_t ic)
 {
     return ((m.n_cats + 64 * ic - 1) / (64 * ic) + 7) / 8 * 8 * (((int64_t)m.n_blocks * m.K + 64 * ic - 1) / (64 * ic));
 }
-// Tiles of 128 x 128 where there are very many (4096 states x 50257: B = 32 389 us against 412 by 64 x 64, B = 256 1020 against 1420); else, where
-// they would cover the GPU in two or three rounds of workgroups, 64 x 64 (512 states: B = 16 58 us against 86, B = 96 97 against 112).
-static bool flow_wide(const pc_mixture &m) { return flow_tiles(m, 2) >= 4096; }
+// Tiles of 128 x 128 where there are very many (128 and 64 wide, us: 3456 tiles, 3440 states x 15645, B = 94 180 and 210, B = 256 318 and 424,
+// with 16 categories a sample 141 and 137); else, where they would cover the GPU in one to three rounds of workgroups, 64 x 64 (1600 tiles,
+// 512 states x 50257: B = 16 87 and 59, B = 94 124 and 106, B = 256 198 and 206, with 16 categories a sample 106 and 77).
+static bool flow_wide(const pc_mixture &m) { return flow_tiles(m, 2) >= 3000; }
 
 // Scratch of the flows: k_flow_prepare's wt, then (from byte `marks` on) its marks, then (from byte `sums` on) the sums of parts.  Preparing pays from some 64 samples on where tiles are
 // wide (4096 states x 50257, B = 64: 64 categories a sample 376 us against 447, gradients without zeros 447 against 450), from 128 where they are not
@@ -789,7 +829,16 @@ using namespace pc;
 
 extern "C" {
 
-pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *stream)
+pc_status pc_predict_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes)
+{
+    const pc_status st = check_mixture(m, B);
+    if (st != PC_OK) return st;
+    if (!bytes) return fail(PC_ERR_ARG, "NULL argument");
+    *bytes = predict_plan(*m, B).bytes;
+    return PC_OK;
+}
+
+pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace, size_t workspace_bytes, void *stream)
 {
     const pc_status st = check_mixture(m, B);
     if (st != PC_OK) return st;
@@ -797,12 +846,15 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
     if (!aligned_to(tables, 16)) return fail(PC_ERR_ARG, "tables must be 16-byte aligned");
     if (ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4)) return fail(PC_ERR_ARG, "logp must be 4-byte aligned");
-    if (m->K >= 4) {
-        launch_predict(*m, tables, B, logp, ld, (hipStream_t)stream);
+    if (m->K < 4) {
+        const dim3 grid((unsigned)((m->n_cats + 63ll) / 64), (unsigned)((B + 63) / 64));
+        hipLaunchKernelGGL(k_predict_any, grid, dim3(256), 0, (hipStream_t)stream, *m, tables, B, logp, ld);
         return launched();
     }
-    const dim3 grid((unsigned)((m->n_cats + 63ll) / 64), (unsigned)((B + 63) / 64));
-    hipLaunchKernelGGL(k_predict_any, grid, dim3(256), 0, (hipStream_t)stream, *m, tables, B, logp, ld);
+    const PredictPlan p = predict_plan(*m, B);
+    if (workspace_bytes < p.bytes) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_workspace_bytes");
+    if (p.bytes && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
+    launch_predict(*m, p, tables, B, logp, ld, p.parts > 1 ? (float *)workspace : nullptr, (hipStream_t)stream);
     return launched();
 }
 

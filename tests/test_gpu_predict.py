@@ -69,7 +69,9 @@ SIZES = [(1, 1, 1, 1), (1, 3, 2, 5), (2, 1, 7, 33), (7, 5, 65, 31), (16, 1, 64, 
          (16, 4, 33000, 40), (20, 3, 32800, 100), (32, 4, 17000, 300), (48, 2, 33000, 65), (128, 1, 4000, 600), (20, 5, 4000, 1200), (100, 1, 3000, 1300),
          (128, 16, 33000, 37), (64, 8, 16411, 2), (128, 16, 32901, 1), (33, 8, 17000, 70),
          # blocks that are no multiple of four states: each remainder, few samples and many, the shortest blocks of the matrix cores
-         (4, 9, 100, 40), (5, 7, 33000, 1), (6, 300, 60, 200), (7, 600, 5000, 33), (9, 5, 33000, 2), (127, 3, 8200, 300), (33, 69, 582, 460), (3, 40, 90, 70)]
+         (4, 9, 100, 40), (5, 7, 33000, 1), (6, 300, 60, 200), (7, 600, 5000, 33), (9, 5, 33000, 2), (127, 3, 8200, 300), (33, 69, 582, 460), (3, 40, 90, 70),
+         # states dealt out to several workgroups: a short last part, one sample, every width of a wave
+         (128, 8, 40, 1), (20, 53, 300, 37), (32, 37, 700, 65), (128, 9, 5001, 129), (100, 13, 130, 300), (64, 18, 20000, 33)]
 
 
 @pytest.mark.parametrize("K,nb,V,B", SIZES)

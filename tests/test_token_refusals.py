@@ -29,7 +29,7 @@ MIXTURE = [(dict(K=0), "PC_ERR_ARG"), (dict(K=129), "PC_ERR_ARG"), (dict(n_block
 @pytest.mark.parametrize("change,want", MIXTURE)
 def test_predict_refuses_mixtures(change, want):
     m = mixture(**change)
-    assert status(pcb.lib().pc_predict(C.byref(m), P, 16, P, 10, None)) == want
+    assert status(pcb.lib().pc_predict(C.byref(m), P, 16, P, 10, None, 0, None)) == want
     assert status(pcb.lib().pc_predict_backward(C.byref(m), P, 16, P, 10, P, 10, 1.0, 1, P, P, 1 << 30, None)) == want
 
 
@@ -38,8 +38,8 @@ def test_predict_refuses_mixtures(change, want):
                                        ((P, 16, P, 9), "PC_ERR_ARG")])
 def test_predict_refuses_arguments(args, want):
     m = mixture()
-    assert status(pcb.lib().pc_predict(C.byref(m), *args, None)) == want
-    assert status(pcb.lib().pc_predict(None, P, 16, P, 10, None)) == "PC_ERR_ARG"
+    assert status(pcb.lib().pc_predict(C.byref(m), *args, P, 1 << 30, None)) == want
+    assert status(pcb.lib().pc_predict(None, P, 16, P, 10, None, 0, None)) == "PC_ERR_ARG"
 
 
 @pytest.mark.parametrize("args", [(P, 9, P, 10, 1.0, 1, P), (P, 10, P, 9, 1.0, 1, P), (None, 10, P, 10, 1.0, 1, P), (P, 10, None, 10, 1.0, 1, P), (P, 10, P, 10, 1.0, 1, None), (P, 10, P, 10, 1.0, 1, P + 4),
@@ -47,6 +47,17 @@ def test_predict_refuses_arguments(args, want):
 def test_predict_backward_refuses_arguments(args):
     m = mixture()
     assert status(pcb.lib().pc_predict_backward(C.byref(m), P, 16, *args, P, 1 << 30, None)) == "PC_ERR_ARG"
+
+
+def test_predict_refuses_workspaces():
+    m, n, L = mixture(n_blocks=64, n_tables=64, n_rows=2048), C.c_size_t(), pcb.lib()
+    assert status(L.pc_predict_workspace_bytes(C.byref(m), 40, C.byref(n))) == "PC_OK" and n.value >= 2 * 40 * 10 * 4
+    for ws, size, want in ((P, n.value - 1, "PC_ERR_WORKSPACE"), (None, 0, "PC_ERR_WORKSPACE"), (None, n.value, "PC_ERR_ARG"), (P + 8, n.value, "PC_ERR_ARG")):
+        assert status(L.pc_predict(C.byref(m), P, 40, P, 10, ws, size, None)) == want
+    assert status(L.pc_predict_workspace_bytes(None, 16, C.byref(n))) == "PC_ERR_ARG"
+    assert status(L.pc_predict_workspace_bytes(C.byref(m), 16, None)) == "PC_ERR_ARG"
+    m = mixture()
+    assert status(L.pc_predict_workspace_bytes(C.byref(m), 16, C.byref(n))) == "PC_OK" and n.value == 0
 
 
 def test_predict_backward_refuses_workspaces():
