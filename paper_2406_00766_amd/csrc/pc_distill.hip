@@ -102,6 +102,15 @@ struct List {
 // maximum and sum per lane: bound by reading it.  Many rows: four waves a row (one where a row is a few packs), so that a CU's
 // other rows cover what follows a row's last load.  Few rows: sixteen.
 constexpr int kPacks = 4;
+// The element (of the grid that begins `off` elements before the row and has `end` up to the row's last) that lane t of a row takes of those
+// in no whole pack; -1: none.
+template <int N>
+__device__ inline int64_t edge_of(int t, int off, int64_t end)
+{
+    const int64_t tail = max(end / N * N, (int64_t)(off > 0 ? N : 0));   // the first element behind the whole packs
+    if (t < N) return off > 0 && t >= off && t < end ? t : -1;
+    return t < 2 * N && tail + t - N < end ? tail + t - N : -1;
+}
 template <typename TS, typename TT, int WAVES, bool LONG>
 __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(const DistillDev d, float *__restrict__ loss, float *__restrict__ stats)
 {
@@ -113,35 +122,42 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(co
         const TS *z = (const TS *)d.student + r * d.student_ld;
         const bool listing = LONG || t < 64;
         List<G, TT> list;
+        float listed[G::LIST], m = PC_NEG_INF_F, s = 0.0f, log_s = 0.0f;
         if (listing) list.fetch(d, r, t);
-        float m = PC_NEG_INF_F, s = 0.0f, log_s = 0.0f;
+        auto look_up = [&]() {                         // while the row is on its way
+            if (!listing) return;
+            list.probabilities(d, lds);
+#pragma unroll
+            for (int i = 0; i < G::LIST; ++i) listed[i] = to_f32(z[max(list.id[i], 0)]);
+        };
         if (!d.normalised) {
-            // packs of the 16-byte grid; the first and last may be cut, their missing elements count as -inf
+            // whole packs of the 16-byte grid, and the elements before the first and behind the last, at most one a lane
             const int off = elements_off(z);
             const TS *grid = z - off;
-            const int64_t end = off + (int64_t)d.n_cats, packs = (end + N - 1) / N;
+            const int64_t end = off + (int64_t)d.n_cats, p_first = off > 0, p_last = end / N;
+            const int64_t edge = edge_of<N>(t, off, end);
             float v[kPacks * N];
             Pack<TS> ahead[kPacks];
-            auto fetch = [&](int64_t p0) {             // whole packs; a pack that is none or cut reads the first whole one that exists, or nothing
+            auto fetch = [&](int64_t p0) {
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k) {
-                    const int64_t i = (p0 + t + k * TH) * N;
-                    if (i >= off && i + N <= end) ahead[k] = *reinterpret_cast<const Pack<TS> *>(__builtin_assume_aligned(grid + i, 16));
+                    const int64_t p = min(p0 + t + k * TH, p_last - 1);
+                    ahead[k] = load_pack((const TS *)__builtin_assume_aligned(grid + p * N, 16));
                 }
             };
-            fetch(0);
-            for (int64_t p0 = 0; p0 < packs; p0 += kPacks * TH) {
-                const bool inner = p0 > 0 && (p0 + kPacks * TH) * N <= end;
+            if (p_first < p_last) fetch(p_first);
+            if (edge >= 0) { m = to_f32(grid[edge]); s = m == PC_NEG_INF_F ? 0.0f : m == m ? 1.0f : m; }
+            look_up();
+            for (int64_t p0 = p_first; p0 < p_last; p0 += kPacks * TH) {
+                const bool whole = p0 + kPacks * TH <= p_last;
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k) {
-                    const int64_t i = (p0 + t + k * TH) * N;
+                    float x[N];
+                    unpack_f32(ahead[k], x);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) v[k * N + e] = to_f32(ahead[k].v[e]);
-                    if (!inner && !(i >= off && i + N <= end))
-#pragma unroll
-                        for (int e = 0; e < N; ++e) v[k * N + e] = i + e >= off && i + e < end ? to_f32(grid[i + e]) : PC_NEG_INF_F;
+                    for (int e = 0; e < N; ++e) v[k * N + e] = whole || p0 + t + k * TH < p_last ? x[e] : PC_NEG_INF_F;
                 }
-                if (p0 + kPacks * TH < packs) fetch(p0 + kPacks * TH);
+                if (p0 + kPacks * TH < p_last) fetch(p0 + kPacks * TH);
                 float top = v[0];
 #pragma unroll
                 for (int e = 1; e < kPacks * N; ++e) top = max2(top, v[e]);
@@ -167,14 +183,14 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(co
             log_s = logf(s);
         } else {
             m = 0.0f;
+            look_up();
         }
         if (!listing) continue;
-        list.probabilities(d, lds);
         float part = 0.0f;
 #pragma unroll
         for (int i = 0; i < G::LIST; ++i)
             if (list.id[i] >= 0 && !(list.q[i] == 0.0f)) {
-                const float v = to_f32(z[list.id[i]]);
+                const float v = listed[i];
                 const float logp = d.normalised ? v : m == PC_NEG_INF_F ? m : (v - m) * d.inv_T - log_s;
                 part += list.q[i] * (list.logq[i] - logp);
             }
@@ -227,7 +243,7 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(co
             Q = shared_Q[sub];
         }
         const bool none = g == 0.0f || Q == 0.0f, zeros = none || d.normalised || m == PC_NEG_INF_F;
-        const float f = Q * expf(-log_s);
+        const float f = g * (Q * expf(-log_s));
         auto dense = [&](float v) { return __builtin_amdgcn_exp2f((v - m) * c) * f; };
         if (listing && !none) {                        // a category listed more than once: its first entry writes for all
 #pragma unroll
@@ -240,36 +256,41 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(co
                     const float oq = LONG ? qs[k] : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.q[0]), k));
                     if (o == list.id[i]) { first = first && k >= j; sum += oq; }
                 }
-                at[i] = g * ((zeros ? 0.0f : dense(at[i])) - sum);
+                at[i] = (zeros ? 0.0f : dense(at[i])) - g * sum;
                 if (!first) list.id[i] = -1;
             }
         }
         const int off = elements_off(out);
         const TS *zg = z - off;                        // element i of the grid is category i - off
         TS *grid = out - off;
-        const int64_t end = off + (int64_t)d.n_cats, packs = (end + N - 1) / N;
-        for (int64_t p0 = 0; p0 < packs; p0 += kPacks * TH) {
-            Pack<TS> in[kPacks];
-            if (!zeros)
+        const int64_t end = off + (int64_t)d.n_cats, p_first = off > 0, p_last = end / N;
+        const int64_t edge = edge_of<N>(t, off, end);
+        if (zeros) {
+            if (edge >= 0) grid[edge] = from_f32<TS>(0.0f);
+            const float x[N] = {};
+            for (int64_t p = p_first + t; p < p_last; p += TH) *reinterpret_cast<Pack<TS> *>(__builtin_assume_aligned(grid + p * N, 16)) = pack_f32<TS>(x);
+        } else {
+            if (edge >= 0) grid[edge] = from_f32<TS>(dense(to_f32(zg[edge])));
+            auto step = [&](int64_t p0, auto some) {   // kPacks of which not all may be there
+                Pack<TS> in[kPacks];
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k) {
-                    const int64_t i = (p0 + t + k * TH) * N;
-                    if (i >= off && i + N <= end) in[k] = load_pack(zg + i);
+                    const int64_t p = p0 + t + k * TH;
+                    in[k] = load_pack(zg + (some ? min(p, p_last - 1) : p) * N);
                 }
 #pragma unroll
-            for (int k = 0; k < kPacks; ++k) {
-                const int64_t i = (p0 + t + k * TH) * N;
-                if (i >= off && i + N <= end) {
+                for (int k = 0; k < kPacks; ++k) {
+                    const int64_t p = p0 + t + k * TH;
                     float x[N];
+                    unpack_f32(in[k], x);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = zeros ? 0.0f : g * dense(to_f32(in[k].v[e]));
-                    *reinterpret_cast<Pack<TS> *>(__builtin_assume_aligned(grid + i, 16)) = pack_f32<TS>(x);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (i + e >= off && i + e < end) grid[i + e] = from_f32<TS>(zeros ? 0.0f : g * dense(to_f32(zg[i + e])));
+                    for (int e = 0; e < N; ++e) x[e] = dense(x[e]);
+                    if (!some || p < p_last) *reinterpret_cast<Pack<TS> *>(__builtin_assume_aligned(grid + p * N, 16)) = pack_f32<TS>(x);
                 }
-            }
+            };
+            int64_t p0 = p_first;
+            for (; p0 + kPacks * TH <= p_last; p0 += kPacks * TH) step(p0, std::false_type{});
+            if (p0 < p_last) step(p0, std::true_type{});
         }
         if (WAVES > 1) __syncthreads();
         else __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");

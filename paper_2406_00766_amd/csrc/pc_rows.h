@@ -33,8 +33,25 @@ template <> __device__ inline bf16_t from_f32<bf16_t>(float v)
 
 // Eight 16-bit or four 32-bit elements, 16 bytes, at any address that suits an element.
 template <typename T> struct Pack { static constexpr int N = 16 / sizeof(T); T v[N]; };
+typedef uint32_t pc_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t pc_u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t pc_u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
-__device__ inline Pack<T> load_pack(const T *p) { Pack<T> r; __builtin_memcpy(&r, p, 16); return r; }
+__device__ inline Pack<T> load_pack(const T *p)       // as one vector: element by element it would be as many loads
+{
+    typedef typename std::conditional<sizeof(T) == 2, pc_u32x4_at2, pc_u32x4_at4>::type loose;
+    return __builtin_bit_cast(Pack<T>, (pc_u32x4)*reinterpret_cast<const loose *>(p));
+}
+template <typename T>
+__device__ inline void unpack_f32(const Pack<T> &r, float (&x)[Pack<T>::N])
+{
+    const pc_u32x4 w = __builtin_bit_cast(pc_u32x4, r);
+#pragma unroll
+    for (int i = 0; i < Pack<T>::N; ++i)
+        if constexpr (std::is_same<T, float>::value) x[i] = __uint_as_float(w[i]);
+        else if constexpr (std::is_same<T, f16_t>::value) x[i] = to_f32(r.v[i]);
+        else x[i] = __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+}
 template <typename T>
 __device__ inline void store_pack(T *p, const Pack<T> &v) { __builtin_memcpy(p, &v, 16); }
 typedef float pc_float2 __attribute__((ext_vector_type(2)));
