@@ -149,7 +149,7 @@ __device__ inline float next_above(float t) { return key_value(order_key(t) + 1)
 // ascending order, ties), the wave raises its bound by the chunk's own maxima, then by its list cut to the n best, and as a last resort
 // passes the chunk through the list an element a lane at a time.  Waves do not wait for each other between the first bound and the end.  Bound
 // by instructions: maximum, exponential, comparison per element (256 x 16 x 50257 bf16, a quarter of the beams at rest: see the table of cases).
-constexpr int kBeamPacks = 4, kWaveList = 256, kBeamWaves = kBeamThreads / 64;
+constexpr int kBeamPacks = 4, kWaveList = 256, kQueue = 128, kBeamWaves = kBeamThreads / 64;
 template <typename T> constexpr int chunk_elements() { return kBeamThreads * kBeamPacks * Pack<T>::N; }
 struct RowPart { float m; float pad; double sum; };    // maximum and sum of exp(z - m) of a segment
 
@@ -189,6 +189,7 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int
 {
     constexpr int N = Pack<T>::N, ELEMS = kBeamPacks * N, CHUNK = chunk_elements<T>();
     __shared__ uint64_t lists[kBeamWaves][kWaveList];
+    __shared__ int32_t queues[kBeamWaves][kQueue];
     __shared__ float nth_lds[kBeamThreads], wave_m[kBeamWaves];
     __shared__ double wave_sum[kBeamWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n_out;
@@ -202,7 +203,31 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int
         const T *grid = z - off;
         const int64_t first = (task % n_seg) * (int64_t)seg_len, hi = min((int64_t)off + a.n_cats, first + seg_len), lo = max((int64_t)off, first);
         float m = PC_NEG_INF_F, sum = 0.0f, t = PC_NEG_INF_F;
+        bool fresh = false;                            // t is reached by n categories of this chunk or before, not above all of them
         WaveList mine{lists[wave], 0};
+        int queued = 0;                                // packs of the wave's queue
+        auto raise = [&]() {                           // the bound above the list's n-th
+            const uint64_t nth = __shfl((unsigned long long)mine.cut(n), n - 1);
+            const float bound = nth ? next_above(key_value((uint32_t)(nth >> 32))) : t;
+            if (bound > t || bound != bound) { t = bound; fresh = false; }
+        };
+        // the queue's elements, a lane each, to the list: all of them, or as many as fill a wave
+        auto drain = [&](bool all) {
+            int head = 0;
+            for (; queued - head >= (all ? 1 : 64 / N); head += 64 / N) {
+                const int at = head + lane / N;
+                const int64_t i = at < queued ? (int64_t)queues[wave][at] * N + lane % N : hi;
+                const bool is = i >= lo && i < hi;
+                const float x = is ? to_f32(grid[i]) : 0.0f;
+                if (mine.count > kWaveList - 64) raise();
+                mine.add(candidate(x, (int)(i - off)), is && (x >= t || t == PC_NEG_INF_F));
+            }
+            queued = max(queued - head, 0);
+            const int32_t rest = lane < queued ? queues[wave][head + lane] : 0;
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+            if (lane < queued) queues[wave][lane] = rest;
+            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        };
         Pack<T> ahead[kBeamPacks];
         auto index = [&](int64_t base, int k) { return base + ((int64_t)k * kBeamThreads + threadIdx.x) * N; };
         auto fetch = [&](int64_t base) {               // whole packs
@@ -217,17 +242,31 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int
 #pragma unroll
             for (int k = 0; k < kBeamPacks; ++k) {
                 const int64_t i = index(base, k);
+                float x[N];
+                unpack_f32(ahead[k], x);
+                if (!inner && !(i >= lo && i + N <= hi)) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[k * N + e] = to_f32(ahead[k].v[e]);
-                if (!inner && !(i >= lo && i + N <= hi))
+                    for (int e = 0; e < N; ++e) x[e] = PC_NEG_INF_F;
+                    if (i < hi && i + N > lo) {        // all its loads at once
+                        T cut[N];
 #pragma unroll
-                    for (int e = 0; e < N; ++e) v[k * N + e] = i + e >= lo && i + e < hi ? to_f32(grid[i + e]) : PC_NEG_INF_F;
+                        for (int e = 0; e < N; ++e) cut[e] = grid[min(max(i + e, lo), hi - 1)];
+#pragma unroll
+                        for (int e = 0; e < N; ++e) x[e] = i + e >= lo && i + e < hi ? to_f32(cut[e]) : PC_NEG_INF_F;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[k * N + e] = x[e];
             }
             if (base + CHUNK < hi) fetch(base + CHUNK);
-            float top = v[0];
+            float tops[kBeamPacks], top = PC_NEG_INF_F;    // NaN: -inf
 #pragma unroll
-            for (int e = 1; e < ELEMS; ++e) top = fmaxf(top, v[e]);
-            top = fmaxf(top, PC_NEG_INF_F);            // NaN alone
+            for (int k = 0; k < kBeamPacks; ++k) {
+                tops[k] = PC_NEG_INF_F;
+#pragma unroll
+                for (int e = 0; e < N; ++e) tops[k] = fmaxf(tops[k], v[k * N + e]);
+                top = fmaxf(top, tops[k]);
+            }
             if (a.normalise) {
                 if (top > m) { sum *= exp2f((m - top) * PC_LOG2E_F); m = top; }
                 const float at = m == PC_NEG_INF_F ? 0.0f : m;
@@ -236,51 +275,34 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int
                 for (int e = 0; e < ELEMS; ++e) part += __builtin_amdgcn_exp2f((v[e] - at) * PC_LOG2E_F);
                 sum += part;
             }
-            bool fresh = false;                        // t is reached by n categories of this chunk or before, not above all of them
-            if (base == first) t = block_nth(top, n, nth_lds), fresh = true;
-            else if (t == PC_NEG_INF_F) t = wave_nth(top, n), fresh = true;
-            bool slow = t == PC_NEG_INF_F;
-            int passing = 0;
-            for (int attempt = 0; !slow; ++attempt) {
-                passing = 0;
-                if (__any(top >= t))
-#pragma unroll
-                    for (int e = 0; e < ELEMS; ++e) passing += __popcll(__ballot(v[e] >= t));
-                if (mine.count + passing <= kWaveList) break;
-                if (attempt == 0) {
-                    const float bound = wave_nth(top, n);
-                    if (!(bound < t)) { t = bound; fresh = true; }
-                } else if (attempt == 1) {
-                    const uint64_t v64 = mine.cut(n), nth = __shfl((unsigned long long)v64, n - 1);
-                    const float bound = nth ? next_above(key_value((uint32_t)(nth >> 32))) : t;
-                    if (bound > t || bound != bound) { t = bound; fresh = false; }
-                } else {
-                    slow = true;
-                }
+            if (base == first) {
+                t = block_nth(top, n, nth_lds);
+                fresh = true;
+            } else if (t == PC_NEG_INF_F || __popcll(__ballot(top >= t)) > 32) {
+                const float bound = wave_nth(top, n);
+                if (!(bound <= t)) { t = bound; fresh = true; }
             }
-            auto category = [&](int e) { return (int)(index(base, e / N) + e % N - off); };
-            if (!slow) {
-                if (passing)
+            if (__any(top >= t)) {
 #pragma unroll
-                    for (int e = 0; e < ELEMS; ++e)
-                        if (__any(v[e] >= t)) mine.add(candidate(v[e], category(e)), v[e] >= t);
-                if (fresh) t = next_above(t);
-            } else {
-                uint64_t above = 0;                    // only keys above this one count
-#pragma unroll 1
-                for (int e = 0; e < ELEMS; ++e) {
-                    if (mine.count > kWaveList - 64) above = __shfl((unsigned long long)mine.cut(n), n - 1);
-                    float x = v[0];
-#pragma unroll
-                    for (int f = 1; f < ELEMS; ++f) x = f == e ? v[f] : x;
-                    const int64_t i = index(base, e / N) + e % N;
-                    const uint64_t key = i >= lo && i < hi ? candidate(x, (int)(i - off)) : 0;
-                    mine.add(key, key > above);
+                for (int k = 0; k < kBeamPacks; ++k) {
+                    const uint64_t those = __ballot(tops[k] >= t);
+                    if (!those) continue;
+                    if (tops[k] >= t) queues[wave][queued + __popcll(those & ((1ull << lane) - 1))] = (int32_t)(index(base, k) / N);
+                    queued += __popcll(those);
+                    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+                    if (queued > kQueue - 64) drain(false);
                 }
-                const uint64_t nth = __shfl((unsigned long long)mine.cut(n), n - 1);
-                t = nth ? next_above(key_value((uint32_t)(nth >> 32))) : PC_NEG_INF_F;
+                if (t == PC_NEG_INF_F) {
+                    drain(true);
+                    if (mine.count >= n) raise();
+                } else if (fresh) {
+                    drain(true);
+                    if (fresh) t = next_above(t);
+                }
+                fresh = false;
             }
         }
+        drain(true);
         uint64_t v = mine.cut(n);
         if (wave > 0) lists[wave][lane] = v;
         float all = m;
