@@ -50,50 +50,37 @@ struct Cand {
     uint64_t key;
     int32_t beam;
 };
-// the value of lane ^ J: within 16 lanes by data-parallel moves, across them by swaps of rows and halves
-template <int J>
-__device__ inline uint32_t lane_xor32(uint32_t v)
-{
-    const int x = (int)v;
-    if constexpr (J == 1) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0xb1, 0xf, 0xf, false);            // quad_perm 1 0 3 2
-    else if constexpr (J == 2) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x4e, 0xf, 0xf, false);       // quad_perm 2 3 0 1
-    else if constexpr (J == 4) {                       // four lanes up for the even fours of a row, four down for the odd ones
-        const int up = __builtin_amdgcn_update_dpp(x, x, 0x104, 0xf, 0x5, false);
-        return (uint32_t)__builtin_amdgcn_update_dpp(up, x, 0x114, 0xf, 0xa, false);
-    } else if constexpr (J == 8) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, false);    // row_ror 8
-    else if constexpr (J == 16) {
-        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        return threadIdx.x & 16 ? r[0] : r[1];
-    } else {
-        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        return threadIdx.x & 32 ? r[0] : r[1];
-    }
-}
-template <int J> __device__ inline float lane_xor(float v) { return __uint_as_float(lane_xor32<J>(__float_as_uint(v))); }
 template <int J> __device__ inline uint64_t lane_xor(uint64_t v) { return (uint64_t)lane_xor32<J>((uint32_t)(v >> 32)) << 32 | lane_xor32<J>((uint32_t)v); }
 __device__ inline bool better(float a, float b) { return a > b; }
 __device__ inline bool better(uint64_t a, uint64_t b) { return a > b; }
 __device__ inline bool better(const Cand &a, const Cand &b) { return a.score > b.score || (a.score == b.score && (a.beam < b.beam || (a.beam == b.beam && a.key > b.key))); }
+// threadIdx.x in a register of its own: conditions on it are made where they are used, not kept for a whole kernel
+__device__ inline uint32_t fresh_lane()
+{
+    uint32_t t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
 // Exchanges over J, J / 2 .. 1 lanes: of a lane and its partner the one whose bit J is clear keeps the better where `up`, the worse elsewhere.
 // Keys are distinct, or equal in all that counts.
 template <int J, typename V>
-__device__ inline V exchanges(const V &v, bool up)
+__device__ __forceinline__ V exchanges(const V &v, bool up)
 {
     const V o = lane_xor<J>(v);
-    const V r = better(o, v) == (((threadIdx.x & J) == 0) == up) ? o : v;
+    const V r = better(o, v) == (((fresh_lane() & J) == 0) == up) ? o : v;
     if constexpr (J > 1) return exchanges<J / 2>(r, up);
     else return r;
 }
 template <int K = 2, typename V>
-__device__ inline V sort_lanes(const V &v)
+__device__ __forceinline__ V sort_lanes(const V &v)
 {
-    const V r = exchanges<K / 2>(v, K == 64 || (threadIdx.x & K) == 0);
+    const V r = exchanges<K / 2>(v, K == 64 || (fresh_lane() & K) == 0);
     if constexpr (K < 64) return sort_lanes<K * 2>(r);
     else return r;
 }
 // The 64 best of two sorted lists; `other` holds the second one in reverse (lane i: its entry 63 - i).
 template <typename V>
-__device__ inline V merge_lanes(const V &v, const V &other)
+__device__ __forceinline__ V merge_lanes(const V &v, const V &other)
 {
     const V r = better(other, v) ? other : v;
     return exchanges<32>(r, true);
@@ -127,8 +114,8 @@ __device__ inline Cand merge_candidates(const Cand &v, const Cand &other)
     return r;
 }
 // n-th largest (n <= 64) of one value per lane of a wave, or per thread of the workgroup.  No NaN.
-__device__ inline float wave_nth(float v, int n) { return __shfl(sort_lanes(v), n - 1); }
-__device__ inline float block_nth(float v, int n, float (&lds)[kBeamThreads])
+__device__ __forceinline__ float wave_nth(float v, int n) { return __shfl(sort_lanes(v), n - 1); }
+__device__ __forceinline__ float block_nth(float v, int n, float (&lds)[kBeamThreads])
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     v = sort_lanes(v);
@@ -149,7 +136,7 @@ __device__ inline float next_above(float t) { return key_value(order_key(t) + 1)
 // ascending order, ties), the wave raises its bound by the chunk's own maxima, then by its list cut to the n best, and as a last resort
 // passes the chunk through the list an element a lane at a time.  Waves do not wait for each other between the first bound and the end.  Bound
 // by instructions: maximum, exponential, comparison per element (256 x 16 x 50257 bf16, a quarter of the beams at rest: see the table of cases).
-constexpr int kBeamPacks = 4, kWaveList = 256, kQueue = 128, kBeamWaves = kBeamThreads / 64;
+constexpr int kBeamPacks = 4, kWaveList = 256, kQueue = 64 * (kBeamPacks + 1), kBeamWaves = kBeamThreads / 64;
 template <typename T> constexpr int chunk_elements() { return kBeamThreads * kBeamPacks * Pack<T>::N; }
 struct RowPart { float m; float pad; double sum; };    // maximum and sum of exp(z - m) of a segment
 
@@ -158,7 +145,7 @@ struct WaveList {
     uint64_t *list;
     int count;
     // the 64 best in order, a lane each; the list becomes the first n of them
-    __device__ inline uint64_t cut(int n)
+    __device__ __forceinline__ uint64_t cut(int n)
     {
         const int lane = threadIdx.x & 63;
         uint64_t v = sort_lanes(lane < count ? list[lane] : 0), nth = __shfl((unsigned long long)v, n - 1);
@@ -184,7 +171,7 @@ struct WaveList {
 };
 
 template <typename T>
-__global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int32_t n_seg, int32_t seg_len, uint64_t *__restrict__ best,
+__global__ __launch_bounds__(kBeamThreads, 5) void k_beam_rows(const BeamDev a, int32_t n_seg, int32_t seg_len, uint64_t *__restrict__ best,
                                                             RowPart *__restrict__ parts)
 {
     constexpr int N = Pack<T>::N, ELEMS = kBeamPacks * N, CHUNK = chunk_elements<T>();
@@ -201,47 +188,31 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int
         const T *z = (const T *)a.scores + r * a.ld;
         const int off = elements_off(z);
         const T *grid = z - off;
-        const int64_t first = (task % n_seg) * (int64_t)seg_len, hi = min((int64_t)off + a.n_cats, first + seg_len), lo = max((int64_t)off, first);
+        const uint32_t first = (uint32_t)(task % n_seg) * (uint32_t)seg_len, hi = min((uint32_t)off + (uint32_t)a.n_cats, first + (uint32_t)seg_len), lo = max((uint32_t)off, first);
         float m = PC_NEG_INF_F, sum = 0.0f, t = PC_NEG_INF_F;
         bool fresh = false;                            // t is reached by n categories of this chunk or before, not above all of them
         WaveList mine{lists[wave], 0};
         int queued = 0;                                // packs of the wave's queue
-        auto raise = [&]() {                           // the bound above the list's n-th
+        auto raise = [&]() __attribute__((always_inline)) {                           // the bound above the list's n-th
             const uint64_t nth = __shfl((unsigned long long)mine.cut(n), n - 1);
             const float bound = nth ? next_above(key_value((uint32_t)(nth >> 32))) : t;
             if (bound > t || bound != bound) { t = bound; fresh = false; }
         };
-        // the queue's elements, a lane each, to the list: all of them, or as many as fill a wave
-        auto drain = [&](bool all) {
-            int head = 0;
-            for (; queued - head >= (all ? 1 : 64 / N); head += 64 / N) {
-                const int at = head + lane / N;
-                const int64_t i = at < queued ? (int64_t)queues[wave][at] * N + lane % N : hi;
-                const bool is = i >= lo && i < hi;
-                const float x = is ? to_f32(grid[i]) : 0.0f;
-                if (mine.count > kWaveList - 64) raise();
-                mine.add(candidate(x, (int)(i - off)), is && (x >= t || t == PC_NEG_INF_F));
-            }
-            queued = max(queued - head, 0);
-            const int32_t rest = lane < queued ? queues[wave][head + lane] : 0;
-            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-            if (lane < queued) queues[wave][lane] = rest;
-            __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-        };
         Pack<T> ahead[kBeamPacks];
-        auto index = [&](int64_t base, int k) { return base + ((int64_t)k * kBeamThreads + threadIdx.x) * N; };
-        auto fetch = [&](int64_t base) {               // whole packs
+        auto index = [&](uint32_t base, int k) { return base + (uint32_t)(k * kBeamThreads + threadIdx.x) * N; };
+        auto fetch = [&](uint32_t base) {               // whole packs
 #pragma unroll
             for (int k = 0; k < kBeamPacks; ++k)
                 if (index(base, k) >= lo && index(base, k) + N <= hi) ahead[k] = *reinterpret_cast<const Pack<T> *>(__builtin_assume_aligned(grid + index(base, k), 16));
         };
         fetch(first);
-        for (int64_t base = first; base < hi; base += CHUNK) {
+        for (uint32_t base = first; base < hi; base += CHUNK) {
             const bool inner = base >= lo && base + CHUNK <= hi;
-            float v[ELEMS];                            // -inf outside [lo, hi)
+            float v[ELEMS], tops[kBeamPacks], top = PC_NEG_INF_F;      // v: -inf outside [lo, hi); tops: no NaN
 #pragma unroll
             for (int k = 0; k < kBeamPacks; ++k) {
-                const int64_t i = index(base, k);
+                tops[k] = PC_NEG_INF_F;
+                const uint32_t i = index(base, k);
                 float x[N];
                 unpack_f32(ahead[k], x);
                 if (!inner && !(i >= lo && i + N <= hi)) {
@@ -256,23 +227,21 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[k * N + e] = x[e];
-            }
-            if (base + CHUNK < hi) fetch(base + CHUNK);
-            float tops[kBeamPacks], top = PC_NEG_INF_F;    // NaN: -inf
-#pragma unroll
-            for (int k = 0; k < kBeamPacks; ++k) {
-                tops[k] = PC_NEG_INF_F;
-#pragma unroll
-                for (int e = 0; e < N; ++e) tops[k] = fmaxf(tops[k], v[k * N + e]);
+                for (int e = 0; e < N; ++e) {
+                    v[k * N + e] = x[e];
+                    tops[k] = fmaxf(tops[k], x[e]);
+                }
                 top = fmaxf(top, tops[k]);
             }
+            if (base + CHUNK < hi) fetch(base + CHUNK);
             if (a.normalise) {
                 if (top > m) { sum *= exp2f((m - top) * PC_LOG2E_F); m = top; }
                 const float at = m == PC_NEG_INF_F ? 0.0f : m;
                 float part = 0.0f;
 #pragma unroll
-                for (int e = 0; e < ELEMS; ++e) part += __builtin_amdgcn_exp2f((v[e] - at) * PC_LOG2E_F);
+                for (int k = 0; k < kBeamPacks; ++k)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) part += __builtin_amdgcn_exp2f((v[k * N + e] - at) * PC_LOG2E_F);
                 sum += part;
             }
             if (base == first) {
@@ -282,27 +251,36 @@ __global__ __launch_bounds__(kBeamThreads) void k_beam_rows(const BeamDev a, int
                 const float bound = wave_nth(top, n);
                 if (!(bound <= t)) { t = bound; fresh = true; }
             }
-            if (__any(top >= t)) {
+            const bool last = base + CHUNK >= hi;
+            if (__any(top >= t) || last) {
 #pragma unroll
                 for (int k = 0; k < kBeamPacks; ++k) {
                     const uint64_t those = __ballot(tops[k] >= t);
                     if (!those) continue;
                     if (tops[k] >= t) queues[wave][queued + __popcll(those & ((1ull << lane) - 1))] = (int32_t)(index(base, k) / N);
                     queued += __popcll(those);
-                    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-                    if (queued > kQueue - 64) drain(false);
                 }
-                if (t == PC_NEG_INF_F) {
-                    drain(true);
-                    if (mine.count >= n) raise();
-                } else if (fresh) {
-                    drain(true);
-                    if (fresh) t = next_above(t);
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+                // the queue's elements, a lane each, to the list: as many as fill a wave, or all where the bound is about to leave them behind
+                const bool all = fresh || last || t == PC_NEG_INF_F;
+                int head = 0;
+                for (; queued - head >= (all ? 1 : 64 / N); head += 64 / N) {
+                    const int at = head + lane / N;
+                    const uint32_t i = at < queued ? (uint32_t)queues[wave][at] * N + lane % N : hi;
+                    const bool is = i >= lo && i < hi;
+                    const float x = is ? to_f32(grid[i]) : 0.0f;
+                    if (mine.count > kWaveList - 64) raise();
+                    mine.add(candidate(x, (int)(i - off)), is && (x >= t || t == PC_NEG_INF_F));
                 }
+                queued = max(queued - head, 0);
+                const int32_t rest = lane < queued ? queues[wave][head + lane] : 0;
+                __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+                if (lane < queued) queues[wave][lane] = rest;
+                if (fresh && t != PC_NEG_INF_F) t = next_above(t);
+                else if (t == PC_NEG_INF_F && mine.count >= n) raise();
                 fresh = false;
             }
         }
-        drain(true);
         uint64_t v = mine.cut(n);
         if (wave > 0) lists[wave][lane] = v;
         float all = m;

@@ -25,14 +25,6 @@ struct DistillDev {                                   // pc_distill without its 
 
 __device__ inline float add2(float a, float b) { return a + b; }
 __device__ inline float max2(float a, float b) { return fmaxf(a, b); }
-template <typename F>
-__device__ inline float wave_all(float v, F op)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v = op(v, __shfl_xor(v, d));
-    return v;
-}
-
 // A row is worked on by WAVES waves of a workgroup.  Its list lies with the first of them where it has at most 64 entries (LONG = false: no
 // barriers), else with all of them, LIST entries a lane.
 constexpr int kShortList = 64;

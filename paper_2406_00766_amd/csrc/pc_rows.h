@@ -77,6 +77,35 @@ __device__ inline Pack<T> pack_f32(const float (&x)[Pack<T>::N])
 template <typename T>
 __device__ inline int elements_off(const T *p) { return (int)(((uintptr_t)p & 15) / sizeof(T)); }
 
+// the value of lane ^ J: within 16 lanes by data-parallel moves, across them by swaps of rows and halves
+template <int J>
+__device__ inline uint32_t lane_xor32(uint32_t v)
+{
+    const int x = (int)v;
+    if constexpr (J == 1) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0xb1, 0xf, 0xf, false);            // quad_perm 1 0 3 2
+    else if constexpr (J == 2) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x4e, 0xf, 0xf, false);       // quad_perm 2 3 0 1
+    else if constexpr (J == 4) {                       // four lanes up for the even fours of a row, four down for the odd ones
+        const int up = __builtin_amdgcn_update_dpp(x, x, 0x104, 0xf, 0x5, false);
+        return (uint32_t)__builtin_amdgcn_update_dpp(up, x, 0x114, 0xf, 0xa, false);
+    } else if constexpr (J == 8) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, false);    // row_ror 8
+    else if constexpr (J == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+}
+template <int J> __device__ inline float lane_xor(float v) { return __uint_as_float(lane_xor32<J>(__float_as_uint(v))); }
+// op over all lanes of a wave, the same in all of them
+template <int J = 32, typename F>
+__device__ inline float wave_all(float v, F op)
+{
+    v = op(v, lane_xor<J>(v));
+    if constexpr (J > 1) return wave_all<J / 2>(v, op);
+    else return v;
+}
+
 inline int64_t type_bytes(int32_t type) { return type == PC_F32 ? 4 : 2; }
 inline bool type_known(int32_t type) { return type == PC_F32 || type == PC_BF16 || type == PC_F16; }
 inline bool aligned_to(const void *p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
