@@ -447,7 +447,8 @@ class mixture:
 
     def __init__(self, weights, K, n_cats, n_blocks, rows=None, table=None, n_tables=None):
         import torch
-        _tensor("weights", weights, torch.float32, (None, None))
+        if not (isinstance(weights, torch.Tensor) and weights.is_cuda and weights.dim() == 2 and _fits(weights, torch.float32, weights.shape, weights.get_device())):
+            _tensor("weights", weights, torch.float32, (None, None))
         self.index, self.columns = weights.get_device(), int(weights.shape[1])
         for name, t in (("rows", rows), ("table", table)):
             if t is not None:
@@ -469,7 +470,8 @@ def pc_get_mixture(handle, var, B, workspace, workspace_bytes) -> mixture:
 def _floats(name, t, n, index):
     """A contiguous float32 tensor of n elements, of any shape."""
     import torch
-    _tensor(name, t, torch.float32, None, index, t.dim() if isinstance(t, torch.Tensor) else 1)
+    if not (isinstance(t, torch.Tensor) and _fits(t, torch.float32, t.shape, index)):
+        _tensor(name, t, torch.float32, None, index, t.dim() if isinstance(t, torch.Tensor) else 1)
     if t.numel() != n:
         _refuse(f"{name} must hold {n} floats, not {t.numel()}")
 

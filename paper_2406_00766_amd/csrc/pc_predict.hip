@@ -216,10 +216,10 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     for (int f = 0; f < FT; ++f) fetch_weights(0, f);
     fetch_tables(0);
 #pragma unroll
-    for (int f = 0; f < FT; ++f) { stage_weights(0, f); fetch_weights(KW, f); }
+    for (int f = 0; f < FT; ++f) { stage_weights(0, f); if (NT > 1 || KW < H) fetch_weights(KW, f); }
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) split_tables(s);
-    fetch_tables(KW);
+    if (NT > 1 || KW < H) fetch_tables(KW);
     __syncthreads();
     // An iteration is STEPS * NT / G slices of 3 G products, among which the work for the next chunk is dealt out: the two waves of a SIMD
     // then find something for the vector ALU while the other one's products run.
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
             for (int q = 0; q < STEPS; ++q) split_tables(q);
             fetch_tables(next);
         };
-        if (NT == 1) {                                 // bound by the loads: they leave first
+        if (NT == 1 && n0 + KW < H) {                  // bound by the loads: they leave first
 #pragma unroll
             for (int f = 0; f < FT; ++f) { stage_weights(buf ^ 1, f); fetch_weights(next, f); }
             tables_on();
