@@ -403,6 +403,12 @@ def _tensor(name, t, dtype=None, shape=None, index=None, last=1):
     return t
 
 
+def _matrix(t, dtype) -> bool:
+    """A contiguous matrix of this type on a GPU."""
+    import torch
+    return isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype is dtype and t.is_contiguous()
+
+
 def _ld(t):
     """Elements between the rows of a matrix (its length where there is but one row, whose stride means nothing)."""
     rows, n = t.shape
@@ -447,7 +453,7 @@ class mixture:
 
     def __init__(self, weights, K, n_cats, n_blocks, rows=None, table=None, n_tables=None):
         import torch
-        if not (isinstance(weights, torch.Tensor) and weights.is_cuda and weights.dim() == 2 and _fits(weights, torch.float32, weights.shape, weights.get_device())):
+        if not _matrix(weights, torch.float32):
             _tensor("weights", weights, torch.float32, (None, None))
         self.index, self.columns = weights.get_device(), int(weights.shape[1])
         for name, t in (("rows", rows), ("table", table)):
@@ -545,7 +551,8 @@ class distill:
 
     def __init__(self, student, ids, teacher, temperature=1.0, teacher_lse=None, normalised=False):
         import torch
-        _tensor("student", student, None, (None, None))
+        if not (isinstance(student, torch.Tensor) and _matrix(student, student.dtype)):
+            _tensor("student", student, None, (None, None))
         self.index = index = student.get_device()
         self.student, self.keep = student, (ids, teacher, teacher_lse)
         self.rows, n_cats = student.shape
@@ -601,7 +608,8 @@ class beam:
 
     def __init__(self, scores, running, n_out, done=None, done_token=0, normalise=False):
         import torch
-        _tensor("scores", scores, None, (None, None))
+        if not (isinstance(scores, torch.Tensor) and _matrix(scores, scores.dtype)):
+            _tensor("scores", scores, None, (None, None))
         self.index = index = scores.get_device()
         if not (isinstance(running, torch.Tensor) and running.dim() == 2 and _fits(running, torch.float32, running.shape, index)):
             _tensor("running", running, torch.float32, (None, None), index, 2)
@@ -635,7 +643,8 @@ def pc_beam_reorder(states, parents, beams, stream=None):
     """For each (src, dst) of `states`: row g * n_out + i of dst = row g * beams + parents[g, i] of src.  Rows are the leading axis;
     a row's elements are contiguous, rows may be strided."""
     import torch
-    _tensor("parents", parents, torch.int32, (None, None), None, 2)
+    if not _matrix(parents, torch.int32):
+        _tensor("parents", parents, torch.int32, (None, None), None, 2)
     groups, n_out = parents.shape
     beams, index = int(beams), parents.get_device()
     if not 1 <= len(states) <= 16:
