@@ -239,14 +239,15 @@ pc_status pc_em_step(pc_circuit *c, float *theta, float *tables, float *theta_fl
  * None of these calls needs a handle: their operands are what the descriptors name, which is read before the call
  * returns and not retained.  They run on the device the calling thread has current.  Like the passes they only
  * enqueue kernels on `stream` and may be captured; a call with no rows (groups) does nothing and returns PC_OK.
- * Workspaces are scratch of one call: nothing in them is kept from call to call, calls that overlap in time need
- * one each. */
+ * Workspaces (16-byte aligned; NULL where none is needed) are scratch of one call: nothing in them is kept from call to call, calls
+ * that overlap in time need one each.  Results do not depend on what a workspace holds, and are the same on every run. */
 enum { PC_F32 = 0, PC_BF16 = 1, PC_F16 = 2 };   /* element types of rows of logits */
 
 /* Input nodes of one variable with their weights in each sample: n_blocks blocks of K nodes; block j's weights are the rows
  * rows[j] .. rows[j] + K - 1 of `weights` (samples contiguous, `stride` floats between rows, stride >= B), its categorical
  * table is tables[table[j]].  rows / table are device arrays of n_blocks entries, or NULL: rows[j] = j * K, table[j] = j.  A
- * block whose rows or table lie outside [0, n_rows) / [0, n_tables) is left out.  The weights are not negative. */
+ * block whose rows or table lie outside [0, n_rows) / [0, n_tables) is left out.  K: 1 .. 128, n_rows >= K.  Weights and table
+ * entries are not negative and at most 2^20 (probabilities).  Tables are 16-byte aligned; samples behind B are not used. */
 typedef struct {
     int32_t K, n_blocks, n_cats, n_tables;
     int64_t n_rows, stride;
@@ -263,7 +264,8 @@ pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void
 
 /* Predictive distribution:  logp[b][c] = log sum_j sum_k weights[rows[j] + k][b] * tables[table[j]][c][k],  b < B, c < n_cats,
  * ld >= n_cats floats between the rows of logp.  A probability below FLT_MIN (a sample without weights: all of them) gives
- * -inf. */
+ * -inf.  Sums are kept in fp32; products are off by at most 3 * 2^-16 of themselves where n_cats >= 4096 (whose
+ * logarithms are large), else 2^-22. */
 pc_status pc_predict_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace,
                      size_t workspace_bytes, void *stream);
@@ -273,7 +275,9 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
  *   flow[t][c][k] = tables[t][c][k] * sum over b and the blocks j of table t of weights[rows[j] + k][b] * dlogp[b][c] / exp(logp[b][c]),
  * which is the objective's gradient with respect to log tables[t][c][k];  table_flow = scale * flow for the tables that the mixture
  * names, added to what is there where `accumulate` is set.  With dlogp = -q (a loss -sum q logp, q >= 0) and scale = -1 these are
- * the flows of an EM step on soft targets, ready for pc_em_step.  Entries of logp below log FLT_MIN add nothing. */
+ * the flows of an EM step on soft targets, ready for pc_em_step.  Entries of logp below log FLT_MIN add nothing.  Sums are kept in
+ * fp32, products are off by at most 2^-22 of themselves.  table_flow is 16-byte aligned, laid out like the tables, and not the tables themselves; flows of tables that
+ * no block names stay as they are. */
 pc_status pc_predict_backward_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t B, const float *logp, int64_t logp_ld,
                               const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow,

@@ -91,8 +91,8 @@ struct List {
 };
 
 // Loss and statistics.  A row passes through registers once, kPacks x 16 bytes a lane at a time, the next ones on their way, with a running
-// maximum and sum per lane: bound by reading it.  Many rows: four waves a row (one where a row is a few packs), so that a CU's
-// other rows cover what follows a row's last load.  Few rows: sixteen.
+// maximum and sum per lane: bound by reading it (8192 x 50257: fp32 270 us, 6.1 TB/s; 16 bits 147, 5.6 TB/s).  The list is made into
+// probabilities, and its student's logits are fetched, while the first packs are on their way.
 constexpr int kPacks = 4;
 // The element (of the grid that begins `off` elements before the row and has `end` up to the row's last) that lane t of a row takes of those
 // in no whole pack; -1: none.
@@ -196,7 +196,8 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(co
 }
 
 // Gradient.  The listed categories' values are made first (from the row itself where the gradient replaces it), then the dense part is
-// written in packs of the output's 16-byte grid, then, behind a barrier, the listed ones over it.
+// written in packs of the output's 16-byte grid, then, behind a barrier, the listed ones over it.  Bound by reading and writing (8192 x
+// 50257: fp32 718 us, 16 bits 358, 4.6 TB/s; a copy reaches 4.9).  Fetching the first packs before the list is made gained nothing.
 template <typename TS, typename TT, int WAVES, bool LONG>
 __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(const DistillDev d, const float *__restrict__ stats,
                                                                                const float *__restrict__ dloss, float scale, void *dstudent, int64_t out_ld)
@@ -318,15 +319,17 @@ static DistillDev distill_dev(const pc_distill *d)
     return DistillDev{d->rows, d->student_ld, d->ids_ld, d->teacher_ld, d->n_cats, d->top, d->student, d->teacher, d->ids, d->teacher_lse,
                       1.0f / d->temperature, d->normalised != 0};
 }
-// f(waves of a row, whether its list is long), as types: one wave where a row is at most 2048 elements, sixteen where there are fewer rows than
-// two a CU, else four.
+// f(waves of a row, whether its list is long), as types: one wave where a row is at most 16 KB, four steps of a wave (one and four waves, us: loss of
+// 20000 x 1000 bf16 25 and 78, of 8192 x 4096 fp32 28 and 33, gradient 65 and 59; of 8192 x 8192 fp32 50 and 48); sixteen where rows are
+// fewer than `few`, else four (sixteen and four: loss of 100 x 50257 fp32 11.4 and 11.5, of 400 24 and 19, gradient of 100 19 and 23,
+// of 400 40 and 43, of 800 x 32000 bf16 33 and 29).
+constexpr int64_t kFewLoss = 128, kFewGrad = 512;
 template <typename F>
-static void with_group(const pc_distill *d, F f)
+static void with_group(const pc_distill *d, int64_t few, F f)
 {
-    const bool long_list = d->top > kShortList;
-    if (long_list) f(Group<4, true>{});
-    else if (d->n_cats <= 2048) f(Group<1, false>{});
-    else if (d->rows < 512) f(Group<16, false>{});
+    if (d->top > kShortList) f(Group<4, true>{});
+    else if (d->n_cats * type_bytes(d->student_type) <= 16384) f(Group<1, false>{});
+    else if (d->rows < few) f(Group<16, false>{});
     else f(Group<4, false>{});
 }
 template <typename G>
@@ -367,7 +370,7 @@ pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t worksp
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            with_group(d, [&](auto g) {
+            with_group(d, kFewLoss, [&](auto g) {
                 using G = decltype(g);
                 hipLaunchKernelGGL((k_distill_rows<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
                                    (hipStream_t)stream, dev, loss, stats);
@@ -391,7 +394,7 @@ pc_status pc_distill_backward(const pc_distill *d, const float *stats, const flo
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            with_group(d, [&](auto g) {
+            with_group(d, kFewGrad, [&](auto g) {
                 using G = decltype(g);
                 hipLaunchKernelGGL((k_distill_grad<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
                                    (hipStream_t)stream, dev, stats, dloss, scale, dstudent, dstudent_ld);

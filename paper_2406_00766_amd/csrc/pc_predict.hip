@@ -104,9 +104,11 @@ __device__ inline floatx16 mfma(const uint4 &a, const uint4 &b, const floatx16 &
 // samples: waves with little to add up, bound by loads in flight) SPLIT waves of a workgroup share categories and add their sums at the end.
 // Each lane fetches its category's table row (8 contiguous states a step of 16, split in registers, read once from memory); the workgroup
 // stages the weights [states][samples] into LDS as planes in operand order.  While a chunk is multiplied the next one is split and staged
-// and the one after it is on its way; one barrier a chunk.  Products of planes down to the last order kept (two planes: hi*hi + hi*lo + lo*hi; three: six).  The samples are the instruction's rows, so that a
-// store covers 32 neighbouring categories.
-// PLANES = 3: all six products down to 2^-24.
+// and the one after it is on its way; one barrier a chunk.  Products of planes down to the last order kept (two planes: hi*hi + hi*lo + lo*hi;
+// three: all six down to 2^-24).  The samples are the instruction's rows, so that a store covers 32 neighbouring categories.  Bound by
+// reading the tables up to some 100 samples (4096 states x 50257: B = 16 173 us, 4.8 TB/s; B = 64 192), then by the matrix cores (B = 256 366 us:
+// 860 TFLOP/s of bf16 products; a large bf16 product reaches 1130).
+// A workgroup adds up `len` states from blockIdx.z * len on; several parts: the sums go to `sums` and k_predict_join takes the logarithm.
 // Where a group of four states begins in the tables and in the weights is looked up in LDS, a window of states at a time, so that
 // blocks need not be as long as a chunk; WHOLE: they are multiples of KC, one look-up serves a wave's part.
 constexpr int kWindow = 2048;
@@ -467,7 +469,7 @@ __global__ __launch_bounds__(256) void k_flow_prepare(const pc_mixture m, int32_
 // Table flows.  A workgroup of 2 x 2 waves owns a tile of 64 I categories x 64 I columns, a column being a node of a block.  The samples are
 // added up 16 at a time from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six
 // products (the terms of a flow have either sign and are few, so that nothing averages out; the fp32 matrix instructions took longer:
-// 4096 states x 50257, B = 256 1372 us against 1020).  While a step is multiplied the next one's operands are split and staged and the one
+// 4096 states x 50257, B = 256, gradients without zeros 1372 us against 1020).  While a step is multiplied the next one's operands are split and staged and the one
 // after is on its way.  Bound by the matrix cores' sustained rate from some 100 samples on (B = 256: six products 557 us), before by reading
 // the tables and writing their flows (B = 32: 389 us, 4.3 TB/s), which the products of a CU's other workgroups cover.
 // MARKED: of every kSegment samples those without gradient among the tile's categories are left out (targets of a few categories a sample:
