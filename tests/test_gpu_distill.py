@@ -172,6 +172,31 @@ def test_masked_and_extreme_student_logits(student, T):
     assert np.isposinf(loss[[3, 4]]).all() and np.isnan(loss[[5, 6]]).all() and loss[7] == 0 and loss[8] == 0 and np.all(grad[8] == 0)
 
 
+@pytest.mark.parametrize("student", list(TYPES))
+@pytest.mark.parametrize("rows,V,pad,in_place", [(9, 5, 0, False), (9, 70, 1, True), (11, 4001, 3, False), (11, 8501, 3, True), (530, 8501, 1, False), (530, 8501, 7, True), (515, 8504, 0, False)])
+def test_ends_of_rows(student, rows, V, pad, in_place):
+    """The elements in no whole 16-byte pack, in rows that start at every offset; one, four and sixteen waves a row."""
+    print(f"case ends {student} rows={rows} V={V} pad={pad}", flush=True)
+    inf = float("inf")
+    z, ids, t, rng = inputs(rows, V, 4, student, "f32", V + pad)
+    ids[:, 0], ids[:, 1] = 0, V - 1
+    z[0, 0] = 30.0
+    z[1, V - 1] = 30.0
+    z[2, 0] = float("nan")
+    z[3, V - 1] = float("nan")
+    z[4, V - 1] = inf
+    z[5, 0] = z[5, V - 1] = -inf
+    z[6, :] = -inf
+    z[6, V - 1] = -4.0                                     # the one category left
+    ids[6, :] = [V - 1, -1, -1, -1]
+    z[7, :] = -inf
+    z[7, 0] = 5.0
+    ids[7, :] = [0, -1, -1, V]
+    z[8, :] = -inf
+    loss, _ = check(z, ids, t, 2.0, pad=pad, in_place=in_place, dloss=torch.from_numpy(rng.random(rows).astype(np.float32) + 0.5))
+    assert np.isnan(loss[[2, 3, 4]]).all() and np.isposinf(loss[[5, 8]]).all() and loss[6] == 0 and loss[7] == 0
+
+
 def test_rows_of_nan_alone_and_teachers_that_are_no_numbers():
     z, ids, t, _ = inputs(4, 90, 5, "f32", "f32", 6)
     z[0, :] = float("nan")
