@@ -33,7 +33,8 @@ def kernel_class(name: str) -> str:
     for prefix, cls in (("k_walk_pass", "sum_fwd"), ("k_split_", "split"), ("k_sum_fwd", "sum_fwd"), ("k_sum_merge", "sum_fwd"), ("k_sum_bwd_child", "sum_bwd_child"), ("k_sum_bwd_small", "sum_bwd_child"),
                         ("k_sum_bwd_param", "sum_bwd_param"), ("k_param_flow", "sum_bwd_param"), ("k_prod_fwd", "prod_fwd"), ("k_prod_tile", "prod_fwd"), ("k_class_bwd", "prod_bwd"),
                         ("k_prod_bwd", "prod_bwd"), ("k_input_fwd", "input_fwd"), ("k_input_bwd", "input_bwd"), ("k_em_", "em"),
-                        ("k_measure_copy", "measure_copy"), ("k_measure_mfma", "measure_mfma")):
+                        ("k_measure_copy", "measure_copy"), ("k_measure_mfma", "measure_mfma"),
+                        ("k_predict", "predict"), ("k_flow_prepare", "predict"), ("k_flow_join", "predict"), ("k_distill", "distill"), ("k_beam", "beam")):
         if n.startswith(prefix):
             return cls
     return "misc"
