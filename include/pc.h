@@ -258,7 +258,7 @@ typedef struct {
 /* The input blocks of variable `var` with their node flows F in a workspace that pc_backward has just filled (same
  * workspace and B as that call, else PC_ERR_STATE).  Where the variable is marginalised the flows are the probabilities of
  * its input nodes given the sample's evidence, so that pc_predict answers p(x_var | evidence).  (In a sample that observes
- * the variable they are the probabilities given that value too.)  Pointers stay valid until the workspace's next pass. */
+ * the variable they are the probabilities given that value too.)  Pointers stay valid until the workspace's next pass, as long as the handle. */
 pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void *workspace, size_t workspace_bytes,
                          pc_mixture *out);
 

@@ -254,3 +254,107 @@ def test_predict_captured_and_replayed_on_changing_inputs():
         g.neg_()
 
     replayed(step, change)
+
+
+@pytest.mark.parametrize("K,nb,V,B", [(32, 6, 1001, 300), (128, 16, 300, 260), (64, 24, 33001, 70), (20, 3, 40, 130)])
+def test_prepared_calls_captured_and_replayed(K, nb, V, B):
+    """Workspaces of the graph's own memory: states and samples in parts, weights by sample, marks that change from replay to replay."""
+    print(f"case capture K={K} blocks={nb} V={V} B={B}", flush=True)
+    full, t = make(K, nb, V, B, 13)
+    w, tables = torch.from_numpy(full).cuda(), torch.from_numpy(t).cuda()
+    m = pcb.mixture(w, K, V, nb)
+    assert max(pcb.pc_predict_workspace_bytes(m, B), pcb.pc_predict_backward_workspace_bytes(m, B)) > 0
+    out, flow, g = torch.empty((B, V), device="cuda"), torch.zeros(t.shape, device="cuda"), torch.randn((B, V), device="cuda")
+    g[torch.rand((B, V), device="cuda") < 0.99] = 0.0
+
+    def step():
+        pcb.pc_predict(m, tables, B, out)
+        pcb.pc_predict_backward(m, tables, B, out, g, 1.0, flow, accumulate=False)
+        return out, flow
+
+    def change():
+        w.copy_(torch.roll(w, 1, 1))
+        g.copy_(torch.roll(g, (1, 7), (0, 1)))
+
+    replayed(step, change)
+
+
+def test_two_streams_at_once_and_workspaces_that_hold_anything():
+    K, nb, V, B = 64, 20, 700, 200
+    cases = []
+    for seed in (21, 22):
+        full, t = make(K, nb, V, B, seed)
+        m, tables = pcb.mixture(torch.from_numpy(full).cuda(), K, V, nb), torch.from_numpy(t).cuda()
+        g = torch.randn((B, V), device="cuda")
+        g[:, : V // 2] = 0.0
+        out, flow = torch.empty((B, V), device="cuda"), torch.empty(t.shape, device="cuda")
+        pcb.pc_predict(m, tables, B, out)
+        pcb.pc_predict_backward(m, tables, B, out, g, 2.0, flow, accumulate=False)
+        sizes = pcb.pc_predict_workspace_bytes(m, B), pcb.pc_predict_backward_workspace_bytes(m, B)
+        assert min(sizes) > 0
+        own = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes]
+        cases.append((m, tables, g, out.clone(), flow.clone(), torch.empty_like(out), torch.empty_like(flow), own))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for s, (m, tables, g, _, _, out, flow, own) in zip(streams, cases):
+            at = s if turn % 2 else s.cuda_stream
+            pcb.pc_predict(m, tables, B, out, stream=at, workspace=own[0] if turn < 3 else None)
+            pcb.pc_predict_backward(m, tables, B, out, g, 2.0, flow, accumulate=False, stream=at, workspace=own[1] if turn < 3 else None)
+        torch.cuda.synchronize()
+        for _, _, _, want_out, want_flow, out, flow, _ in cases:
+            assert torch.equal(out, want_out) and torch.equal(flow, want_flow)
+            out.zero_()
+            flow.zero_()
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("B", [3, 70, 200])
+def test_flows_where_a_sample_has_only_tiny_table_entries(B):
+    """p near FLT_MIN: W g / p is as large as g over the entry, the flow itself about g."""
+    K, V = 32, 5
+    full, t = make(K, 2, V, B, 31)
+    t[:, 2, :] *= np.float32(1e-36)
+    table = np.arange(2, dtype=np.int32)
+    p = exact_p(full, t, B, [0, K], table)
+    logp = np.log(p).astype(np.float32)
+    assert logp[:, 2].max() < -80 and logp.min() > -87
+    g = np.zeros((B, V), np.float32)
+    g[:, 2] = -np.linspace(0.01, 1.0, B, dtype=np.float32)
+    flow = torch.empty(t.shape, device="cuda")
+    pcb.pc_predict_backward(pcb.mixture(torch.from_numpy(full).cuda(), K, V, 2), torch.from_numpy(t).cuda(), B, torch.from_numpy(logp).cuda(), torch.from_numpy(g).cuda(), -1.0,
+                            flow, accumulate=False)
+    r = g / np.exp(logp.astype(np.float64))
+    want = -np.stack([(full[j * K:(j + 1) * K, :B].astype(np.float64) @ r).T for j in range(2)]) * t
+    check_flow(flow.cpu().numpy().astype(np.float64), want, want, B)
+
+
+@pytest.mark.parametrize("B", [1, 3, 70, 130])
+def test_offsets_beyond_32_bits(B):
+    """Tables of more than 4 GiB, rows of log-probabilities and of gradients that begin more than 2^31 elements into their memory."""
+    K, V, far = 128, 50257, 168
+    print(f"case far B={B}", flush=True)
+    rng = np.random.default_rng(41)
+    near = torch.from_numpy((rng.random((2, V, K)) / V).astype(np.float32)).cuda()
+    full, _ = make(K, 2, 2, B, 42)
+    w = torch.from_numpy(full).cuda()
+    tables, flow = torch.empty((far + 1, V, K), device="cuda"), torch.empty((far + 1, V, K), device="cuda")
+    assert tables.numel() > 1 << 30
+    tables[0], tables[far] = near[0], near[1]
+    flow[1:far].fill_(4.0)
+    table = torch.tensor([0, far], dtype=torch.int32, device="cuda")
+    m, small = pcb.mixture(w, K, V, 2, table=table, n_tables=far + 1), pcb.mixture(w, K, V, 2)
+    ld = max(V, (1 << 31) // max(B - 1, 1) + 1) if B > 1 else V
+    hold = torch.empty((B - 1) * ld + V, device="cuda")
+    logp, want = hold.as_strided((B, V), (ld, 1)), torch.empty((B, V), device="cuda")
+    pcb.pc_predict(m, tables, B, logp)
+    pcb.pc_predict(small, near, B, want)
+    assert torch.equal(logp, want)
+    hold_g = torch.empty((B - 1) * ld + V, device="cuda")
+    g = hold_g.as_strided((B, V), (ld, 1))
+    g.copy_(torch.where(torch.rand((B, V), device="cuda") < 0.01, 1.0, 0.0))
+    want_flow = torch.empty_like(near)
+    pcb.pc_predict_backward(small, near, B, want, g.contiguous(), 1.0, want_flow, accumulate=False)
+    pcb.pc_predict_backward(m, tables, B, logp, g, 1.0, flow, accumulate=False)
+    assert torch.allclose(flow[0], want_flow[0], rtol=2.0 ** -20, atol=0) and torch.allclose(flow[far], want_flow[1], rtol=2.0 ** -20, atol=0)
+    assert bool((flow[1:far] == 4.0).all())
