@@ -114,8 +114,9 @@ __device__ inline floatx16 mfma(const uint4 &a, const uint4 &b, const floatx16 &
 constexpr int kWindow = 2048;
 template <int NT, int WAVES, int SPLIT, int KC, int PLANES, bool WHOLE>
 __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 3 : 4) void k_predict(const pc_mixture m, const float *__restrict__ tables, int32_t B,
-                                                                        float *__restrict__ logp, int64_t ld, int32_t len, float *__restrict__ sums)
+                                                                        float *__restrict__ logp, int64_t ld, int32_t len, float *__restrict__ sums, const pc_u32x4 *__restrict__ ready)
 {
+    constexpr bool READY = NT >= 4;
     constexpr int TH = 64 * WAVES, NB = 32 * NT, STEPS = KC / 16, KW = KC * SPLIT, TASKS = NB * KW / 8, FT = (TASKS + TH - 1) / TH;
     __shared__ uint4 planes[2][PLANES][KW / 8][NB];   // [buffer][plane][8 states][sample]
     __shared__ int64_t t_at[kWindow / 4], w_at[kWindow / 4];
@@ -152,10 +153,18 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     // What lies outside (blocks left out, states behind the last, samples behind B) is read from a place that exists and masked when it is
     // split.  A chunk behind the last state is fetched and staged like any other, and not used.
     Pack<float> t_raw[STEPS][2];
-    float w_raw[FT][8];
+    float w_raw[READY ? 1 : FT][8];
+    pc_u32x4 w_ready[READY ? FT : 1][PLANES];
+    const int columns = gridDim.y * NB, groups = (m.n_blocks * Kg + 7) / 8;
     uint32_t t_mask[WHOLE ? 1 : STEPS][2];
     int w_skip[FT][2];                                 // 4: all
-    auto fetch_weights = [&](int n0, int f) {          // of the chunk that begins with state `first` + n0
+    auto fetch_weights = [&](int n0, int f) {
+        if (READY) {
+            const int g = min((first + n0) / 8 + task_g[f], groups - 1);
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) w_ready[f][p] = (ready + ((int64_t)p * groups + g) * columns)[b0 + task_b[f]];
+            return;
+        }          // of the chunk that begins with state `first` + n0
         const int g0 = n0 % kWindow / 4;
         if (!wave_stages[f]) return;
         const int b = min(task_b[f], here - 1);
@@ -192,6 +201,11 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     };
     auto masked = [](float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask) * kUp; };
     auto stage_weights = [&](int buf, int f) {
+        if (READY) {
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) planes[buf][p][task_g[f]][task_b[f]] = __builtin_bit_cast(uint4, w_ready[f][p]);
+            return;
+        }
         if (!wave_stages[f]) return;
         float x[8];
         uint4 pl[PLANES];
@@ -302,6 +316,31 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
                 else logp[(int64_t)b * ld + c0 + col] = log_p(p);
             }
         }
+}
+
+// The weights as planes in operand order, ready[plane][8 states][sample]: what k_predict with wide waves stages as it is.
+template <int PLANES>
+__global__ __launch_bounds__(256) void k_predict_ready(const pc_mixture m, int32_t B, int32_t columns, uint4 *__restrict__ ready)
+{
+    const int Kg = group_states(m.K), groups = (m.n_blocks * Kg + 7) / 8, b = blockIdx.y * 64 + threadIdx.x % 64, g = blockIdx.x * 4 + threadIdx.x / 64;
+    if (g >= groups || b >= columns) return;
+    float x[8];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const int n = 8 * g + 4 * q;
+        const MixBlock blk = b < B && n < m.n_blocks * Kg ? mix_block(m, n / Kg) : MixBlock{-1, -1};
+        const int k = group_start(m.K, n % Kg), skip = blk.row >= 0 ? n % Kg - k : 4;
+        const float *src = m.weights + (blk.row >= 0 ? (blk.row + k) * m.stride + b : 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float v = src[blk.row >= 0 ? i * m.stride : 0];
+            x[4 * q + i] = i >= skip ? v * kUp : 0.0f;
+        }
+    }
+    uint4 pl[PLANES];
+    split8(x, pl);
+#pragma unroll
+    for (int p = 0; p < PLANES; ++p) ready[((int64_t)p * groups + g) * columns + b] = pl[p];
 }
 
 // Log-probabilities from the sums over `parts` parts of the states.
@@ -729,7 +768,7 @@ static int64_t few_rows(const pc_mixture &m) { return 64 / ((m.K + 3) / 4) * kFe
 // Where there is less than a workgroup to a CU and the states are many (1024: an exchange and a second launch take some 4 us) they are dealt out
 // in parts of at least 256, as many as fill the GPU once, whose sums k_predict_join adds up (4096 states x 256, B = 256 22 us against 61;
 // x 5000 63 against 144; x 16000, 2048 states, B = 500 124 against 135; with more workgroups, 1024 states x 50257, B = 64 66 against 49).
-struct PredictPlan { bool few, exact; int32_t nt, len, parts; size_t bytes; };
+struct PredictPlan { bool few, exact; int32_t nt, len, parts, columns; size_t sums, bytes; };
 static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
 {
     PredictPlan p{};
@@ -746,11 +785,13 @@ static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
     const int64_t want = groups < 256 ? std::min(slots / groups, most) : 1;
     p.len = (int32_t)((H + want * 128 - 1) / (want * 128) * 128);
     p.parts = (int32_t)((H + p.len - 1) / p.len);
-    p.bytes = p.parts > 1 ? (size_t)p.parts * B * m.n_cats * 4 : 0;
+    p.columns = (int32_t)(columns() * 32 * p.nt);
+    p.sums = p.nt >= 4 ? (size_t)(p.exact ? 3 : 2) * ((H + 7) / 8) * p.columns * 16 : 0;
+    p.bytes = p.sums + (p.parts > 1 ? (size_t)p.parts * B * m.n_cats * 4 : 0);
     return p;
 }
 
-static void launch_predict(const pc_mixture &m, const PredictPlan &p, const float *tables, int32_t B, float *logp, int64_t ld, float *sums, hipStream_t s)
+static void launch_predict(const pc_mixture &m, const PredictPlan &p, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace, hipStream_t s)
 {
     if (p.few) {
         const dim3 grid((unsigned)((m.n_cats + 4 * few_rows(m) - 1) / (4 * few_rows(m))));
@@ -759,11 +800,19 @@ static void launch_predict(const pc_mixture &m, const PredictPlan &p, const floa
         return;
     }
     const int64_t rows = (m.n_cats + 31ll) / 32;
+    uint4 *ready = (uint4 *)workspace;
+    float *sums = p.parts > 1 ? (float *)((char *)workspace + p.sums) : nullptr;
+    if (p.nt >= 4) {
+        const int64_t groups = ((int64_t)m.n_blocks * ((m.K + 3) / 4 * 4) + 7) / 8;
+        const dim3 grid((unsigned)((groups + 3) / 4), (unsigned)((p.columns + 63) / 64));
+        if (p.exact) hipLaunchKernelGGL(k_predict_ready<3>, grid, dim3(256), 0, s, m, B, p.columns, ready);
+        else hipLaunchKernelGGL(k_predict_ready<2>, grid, dim3(256), 0, s, m, B, p.columns, ready);
+    }
 #define PC_PREDICT(NT, WAVES, SPLIT, KC, PLANES)                                                                               \
     if (p.nt == NT && p.exact == (PLANES == 3)) {                                                                              \
         const dim3 grid((unsigned)((rows + WAVES / SPLIT - 1) / (WAVES / SPLIT)), (unsigned)((B + 32 * NT - 1) / (32 * NT)), p.parts);  \
-        if (m.K % KC == 0) hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, true>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums); \
-        else hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, false>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums); \
+        if (m.K % KC == 0) hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, true>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums, (const pc_u32x4 *)ready); \
+        else hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, false>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums, (const pc_u32x4 *)ready); \
     }
     PC_PREDICT(8, 8, 1, 32, 2)
     PC_PREDICT(4, 4, 1, 32, 2)
@@ -856,7 +905,7 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
     const PredictPlan p = predict_plan(*m, B);
     if (workspace_bytes < p.bytes) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_workspace_bytes");
     if (p.bytes && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
-    launch_predict(*m, p, tables, B, logp, ld, p.parts > 1 ? (float *)workspace : nullptr, (hipStream_t)stream);
+    launch_predict(*m, p, tables, B, logp, ld, workspace, (hipStream_t)stream);
     return launched();
 }
 
