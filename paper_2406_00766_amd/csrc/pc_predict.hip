@@ -462,24 +462,35 @@ __device__ inline void flow_column(const pc_mixture &m, int n, int64_t &w_at, in
     more = again;
 }
 
-// What k_predict_flow<MARKED> reads: the weights by sample, wt[b][n], a table's further blocks added to its first one's column, in the
-// first `turns` workgroups, 64 columns x 64 samples each; in the others marks, a wave for 64 categories and 32 samples: bit b % 32 of
-// marks[c / 64][b / 32] is set where sample b has a gradient that is not zero among those categories.
-__global__ __launch_bounds__(256) void k_flow_prepare(const pc_mixture m, int32_t B, const float *__restrict__ dlogp, int64_t ld, int32_t turns, float *__restrict__ wt,
-                                                      uint32_t *__restrict__ marks)
+// What k_predict_flow<MARKED> reads, in its workspace.  Samples are dealt out in parts of `part` (several where tiles are few), looked at kSegment at a time.
+constexpr int kSegment = 512;
+struct FlowPrep {
+    float *wt;                                         // weights by sample, [B][H], a table's further blocks added to its first one's column
+    uint32_t *marks;                                   // bit b % 32 of [c / 64][b / 32]: sample b has a gradient that is not zero among 64 categories
+    pc_u32x4 *wp, *rp;                                 // planes of the weights [8 samples][plane][H] and of g / p [8 samples][plane][n_cats]; zeros behind B
+    float *sums;                                       // [part][n_cats][H], or NULL: one part
+    int32_t part;
+};
+__device__ inline bool mostly(int count, int of) { return count * 4 > of * 3; }
+// The first `turns` workgroups: weights, 64 columns x 64 samples each.  The others: a segment of 64 I categories each, its marks, and g / p where
+// most of its samples count.
+constexpr int kPrepareWaves = 8;
+template <int I>
+__global__ __launch_bounds__(64 * kPrepareWaves) void k_flow_prepare(const pc_mixture m, int32_t B, const float *__restrict__ logp, int64_t lp_ld, const float *__restrict__ dlogp,
+                                                      int64_t ld, int32_t turns, const FlowPrep f)
 {
     __shared__ float x[64][65];
     __shared__ int64_t w_at[64], o_at[64];
     __shared__ int32_t more[64];
+    __shared__ uint32_t bits[I][kSegment / 32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = m.n_blocks * m.K;
     if ((int)blockIdx.x < turns) {
         const int n0 = blockIdx.x % ((H + 63) / 64) * 64, b0 = blockIdx.x / ((H + 63) / 64) * 64, b = min(b0 + lane, B - 1);
         if (wave == 0) flow_column(m, n0 + lane, w_at[lane], o_at[lane], more[lane]);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[wave + 4 * i][lane] = m.weights[max(w_at[wave + 4 * i], (int64_t)0) + b];
-        for (int i = 0; i < 16; ++i) {
-            const int c = wave + 4 * i;
+        for (int c = wave; c < 64; c += kPrepareWaves) x[c][lane] = m.weights[max(w_at[c], (int64_t)0) + b];
+        for (int c = wave; c < 64; c += kPrepareWaves) {
             if (m.table && w_at[c] >= 0 && more[c])
                 for (int o = (n0 + c) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
                     const MixBlock blk = mix_block(m, o);
@@ -487,47 +498,89 @@ __global__ __launch_bounds__(256) void k_flow_prepare(const pc_mixture m, int32_
                 }
         }
         __syncthreads();
-        for (int i = 0; i < 16; ++i) {
-            const int s = wave + 4 * i;
-            if (b0 + s < B && n0 + lane < H) wt[(int64_t)(b0 + s) * H + n0 + lane] = x[lane][s];
+        if (n0 + lane >= H) return;
+        for (int s = wave; s < 64; s += kPrepareWaves) {
+            if (b0 + s < B) f.wt[(int64_t)(b0 + s) * H + n0 + lane] = x[lane][s];
+        }
+        for (int g = wave; g < 8 && b0 + 8 * g < (B + 15) / 16 * 16; g += kPrepareWaves) {
+            float v[8];
+            uint4 pl[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = b0 + 8 * g + e < B ? x[lane][8 * g + e] * kUp : 0.0f;
+            split8(v, pl);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) f.wp[((int64_t)(b0 / 8 + g) * 3 + p) * H + n0 + lane] = __builtin_bit_cast(pc_u32x4, pl[p]);
         }
         return;
     }
-    const int64_t rows = (m.n_cats + 63ll) / 64, words = (B + 31ll) / 32, job = (int64_t)(blockIdx.x - turns) * 4 + wave;
-    if (job >= rows * words) return;
-    const int64_t row = job % rows, word = job / rows, c = min(row * 64 + lane, (int64_t)m.n_cats - 1);
-    float g[32];
+    const int64_t rows = (m.n_cats + 63ll) / 64, words = (B + 31ll) / 32, tiles = (rows + I - 1) / I, job = blockIdx.x - turns, row0 = job % tiles * I;
+    const int64_t segments = (f.part + kSegment - 1) / kSegment, at = job / tiles, s0 = at / segments * f.part + at % segments * kSegment;
+    const int here = (int)min(min((int64_t)B, (at / segments + 1) * f.part) - s0, (int64_t)kSegment);
+    if (here <= 0) return;
+    for (int j = wave; j < (here + 31) / 32 * I; j += kPrepareWaves) {
+        const int64_t row = row0 + j % I, b0 = s0 + j / I * 32, c = min(row * 64 + lane, (int64_t)m.n_cats - 1);
+        uint32_t w = 0;
+        if (row < rows) {
+            float g[32];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) g[e] = dlogp[min(word * 32 + e, (int64_t)B - 1) * ld + c];
-    uint32_t bits = 0;
+            for (int e = 0; e < 32; ++e) g[e] = dlogp[min(b0 + e, (int64_t)B - 1) * ld + c];
 #pragma unroll
-    for (int e = 0; e < 32; ++e) bits |= (__ballot(g[e] != 0.0f) != 0 && word * 32 + e < B ? 1u : 0u) << e;
-    if (lane == 0) marks[row * words + word] = bits;
+            for (int e = 0; e < 32; ++e) w |= (__ballot(g[e] != 0.0f) != 0 && b0 + e < B ? 1u : 0u) << e;
+            if (lane == 0) f.marks[row * words + b0 / 32] = w;
+        }
+        if (lane == 0) bits[j % I][j / I] = w;
+    }
+    __syncthreads();
+    int count = 0;
+    for (int j = 0; j < (here + 31) / 32; ++j) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < I; ++i) w |= bits[i][j];
+        count += __popc(w);
+    }
+    if (!mostly(count, here)) return;
+    for (int j = wave; j < (here + 15) / 16 * 2 * I; j += kPrepareWaves) {
+        const int64_t c = (row0 + j % I) * 64 + lane, b0 = s0 + j / I * 8;
+        if (c >= m.n_cats) continue;
+        float l[8], d[8], v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t b = min(b0 + e, (int64_t)B - 1);
+            l[e] = logp[b * lp_ld + c];
+            d[e] = dlogp[b * ld + c];
+        }
+        uint4 pl[3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = b0 + e < B ? flow_ratio(l[e], d[e]) : 0.0f;
+        split8(v, pl);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) f.rp[((b0 / 8) * 3 + p) * m.n_cats + c] = __builtin_bit_cast(pc_u32x4, pl[p]);
+    }
 }
 
 // Table flows.  A workgroup of 2 x 2 waves owns a tile of 64 I categories x 64 I columns, a column being a node of a block.  The samples are
 // added up 16 at a time from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six
 // products (the terms of a flow have either sign and are few, so that nothing averages out; the fp32 matrix instructions took longer:
-// 4096 states x 50257, B = 256, gradients without zeros 1372 us against 1020).  While a step is multiplied the next one's operands are split and staged and the one
-// after is on its way.  Bound by the matrix cores' sustained rate from some 100 samples on (B = 256: six products 557 us), before by reading
-// the tables and writing their flows (B = 32: 389 us, 4.3 TB/s), which the products of a CU's other workgroups cover.
-// MARKED: of every kSegment samples those without gradient among the tile's categories are left out (targets of a few categories a sample:
-// an EM step; 64 categories a sample, B = 256 445 us against 967 with all of them), except where few would be; the weights are those of
-// k_flow_prepare, by sample, so that the columns of any sample are neighbours (gathered from the rows of m.weights: 737 us).
+// 4096 states x 50257, B = 256, gradients without zeros 1372 us).  While a step is multiplied the next one's operands are staged and the one
+// after is on its way.  Bound by the matrix cores' sustained rate from some 100 samples on (B = 256: 795 us, six products alone 557; making the
+// planes in every tile took 1010), before by reading the tables and writing their flows (B = 32: 371 us, 4.5 TB/s), which the products of a
+// CU's other workgroups cover.
+// MARKED: operands as k_flow_prepare has left them.  Of a segment whose samples mostly have no gradient among the tile's categories (targets of
+// a few categories a sample: an EM step) only those that do are added up, their g / p made here and their weights taken by sample,
+// so that the columns of any sample are neighbours (64 categories a sample, B = 256: 438 us; gathered from the rows of m.weights 737,
+// all samples 967).
 // LISTS: a table named by several blocks is the first one's: its column adds up all their weights, the others' columns do nothing, so every entry has
 // one writer.  The workgroups of a category tile follow one another on one XCD, whose cache keeps its g / p.
-constexpr int kSegment = 512;
 template <int I, bool MARKED, bool LISTS>
 __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_mixture m, const float *__restrict__ tables, int32_t B, const float *__restrict__ logp,
                                                          int64_t lp_ld, const float *__restrict__ dlogp, int64_t dl_ld, float scale, int32_t accumulate,
-                                                         float *__restrict__ flow, const float *__restrict__ wt, const uint32_t *__restrict__ marks, int32_t part, float *__restrict__ sums)
+                                                         float *__restrict__ flow, const FlowPrep f)
 {
     constexpr int TH = 256, TC = 64 * I, TN = 64 * I, NP = TN + 4;   // four more: the two groups of a column lie in other banks
     __shared__ uint4 rs[2][3][2][TC], ws[2][3][2][NP];                            // [buffer][plane][8 samples][category or column]
     __shared__ int64_t w_at[TN], o_at[TN];            // first weight of a column, -1: none; its place in the flows for category 0
     __shared__ int32_t more[TN];                      // the column's table has further blocks
     __shared__ uint16_t list[MARKED ? kSegment : 1];    // samples of the segment that count
-    __shared__ int32_t n_list;
     const int H = m.n_blocks * m.K, n_tiles = (H + TN - 1) / TN, q = blockIdx.x / 8;
     const int64_t c0 = ((int64_t)(q / n_tiles) * 8 + blockIdx.x % 8) * TC;
     const int n0 = q % n_tiles * TN;
@@ -535,6 +588,16 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
     const int64_t mark_rows = (m.n_cats + 63ll) / 64, mark_ld = (B + 31ll) / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int cw = wave / 2 * 32 * I, nw = wave % 2 * 32 * I;
+    const int first = MARKED ? blockIdx.y * f.part : 0, last = MARKED ? min(B, first + f.part) : B;
+    auto marks_of = [&](int s0, int here) {
+        uint32_t w = 0;
+        if (32 * lane < here)
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                if (c0 / 64 + i < mark_rows) w |= f.marks[(c0 / 64 + i) * mark_ld + s0 / 32 + lane];
+        return w;
+    };
+    const uint32_t first_word = MARKED ? marks_of(first, min(kSegment, last - first)) : 0;
     for (int i = threadIdx.x; i < TN; i += TH) flow_column(m, n0 + i, w_at[i], o_at[i], more[i]);
     __syncthreads();
     // What a thread stages a step: eight samples of a category (the group of samples is the wave's), and of a column (two lanes read 16 samples
@@ -542,10 +605,9 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
     static_assert(I == 1 || I == 2, "the dealing below");
     const bool of_ratios = I == 2 || wave < 2, of_weights = I == 2 || wave >= 2;
     const int r_group = I == 2 ? wave / 2 : wave % 2, r_cat = I == 2 ? threadIdx.x % TC : lane;
-    const int64_t cat = min(c0 + r_cat, (int64_t)m.n_cats - 1);
     const int w_col = MARKED ? (I == 2 ? threadIdx.x % TN : lane) : threadIdx.x % (I == 2 ? TH : TH / 2) / 2;
     const int w_group = MARKED ? r_group : lane % 2;
-    const float *w_row = MARKED ? wt + min(n0 + w_col, H - 1) : m.weights + max(w_at[w_col], (int64_t)0);
+    const float *w_row = MARKED ? f.wt : m.weights + max(w_at[w_col], (int64_t)0);
     const bool w_more = LISTS && w_at[w_col] >= 0 && more[w_col];
     floatx16 acc[I][I];
 #pragma unroll
@@ -555,42 +617,56 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][k][e] = 0.0f;
     bool none = true;                                  // no sample counts for this tile
-    const int first = MARKED ? blockIdx.y * part : 0, last = MARKED ? min(B, first + part) : B;
+    // READY: the segments whose operands are as k_flow_prepare has left them; else the others.  Each way has its own loop: its registers are its own.
+    auto pass = [&](auto as_ready) {
+    constexpr bool READY = decltype(as_ready)::value;
     for (int s0 = first; s0 < last; s0 += MARKED ? kSegment : B) {
         const int here = MARKED ? min(kSegment, last - s0) : B;
-        bool all = true;
-        if (MARKED) {                                  // the samples that count, in order
-            __syncthreads();
-            if (wave == 0) {
-                int n = 0;
-                for (int b = 0; b < here; b += 64) {
-                    uint64_t those = 0;
-                    for (int i = 0; i < I; ++i)
-                        for (int h = 0; h < 2; ++h)
-                            if (b + 32 * h < here && c0 / 64 + i < mark_rows)
-                                those |= (uint64_t)marks[(c0 / 64 + i) * mark_ld + (s0 + b) / 32 + h] << 32 * h;
-                    if (those >> lane & 1) list[n + __popcll(those & ((1ull << lane) - 1))] = (uint16_t)(b + lane);
-                    n += __popcll(those);
-                }
-                if (lane == 0) n_list = n;
+        int n_samples = here;
+        if (MARKED) {
+            // lane i has the marks of samples 32 i to 32 i + 31; the list is made of them in order
+            const uint32_t word = s0 == first ? first_word : marks_of(s0, here);
+            int n = 0;
+#pragma unroll
+            for (int j = 0; j < kSegment / 32; ++j) n += __popc(__builtin_amdgcn_readlane(word, j));
+            if (mostly(n, here) != READY || n == 0) continue;
+            if (!READY) {
+                n_samples = n;
+                __syncthreads();                       // the list before is read
+                if (wave == 0)
+                    for (int j = 0, at = 0; j < (here + 31) / 32; ++j) {
+                        const uint32_t those = __builtin_amdgcn_readlane(word, j);
+                        if (lane < 32 && those >> lane & 1) list[at + __popc(those & ((1u << lane) - 1))] = (uint16_t)(32 * j + lane);
+                        at += __popc(those);
+                    }
+                __syncthreads();
             }
-            __syncthreads();
-            all = n_list * 4 > here * 3;
         }
-        const int n_samples = all ? here : n_list;
-        if (n_samples == 0) continue;
         none = false;
-        auto sample = [&](int i) { return s0 + (!MARKED || all ? i : list[i]); };
-        float l[8], d[8], w[8];
+        int cat = (int)min(c0 + r_cat, (int64_t)m.n_cats - 1), w_n = min(n0 + w_col, H - 1);
+        if (MARKED) asm volatile("" : "+v"(cat), "+v"(w_n));     // addresses are made here, not kept for both ways
+        auto sample = [&](int i) { return s0 + (!MARKED ? i : list[i]); };
+        float l[READY ? 1 : 8], d[READY ? 1 : 8], w[READY ? 1 : 8];
+        pc_u32x4 r_ready[3], w_ready[3];
+        auto group = [&](int i, int which) { return (int64_t)min((s0 + i) / 8 + which, (B + 15) / 16 * 2 - 1) * 3; };
         auto fetch_ratios = [&](int i0) {
+            if constexpr (READY) {
+#pragma unroll
+                for (int p = 0; p < 3; ++p) r_ready[p] = f.rp[(group(i0, r_group) + p) * m.n_cats + cat];
+            } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int64_t at = __builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * r_group + e, n_samples - 1)));
                 l[e] = (logp + at * lp_ld)[cat];
                 d[e] = (dlogp + at * dl_ld)[cat];
             }
+            }
         };
         auto stage_ratios = [&](int i0, int buf) {
+            if constexpr (READY) {
+#pragma unroll
+                for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = __builtin_bit_cast(uint4, r_ready[p]);
+            } else {
             float x[8];
             uint4 pl[3];
 #pragma unroll
@@ -601,6 +677,7 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
             split8(x, pl);
 #pragma unroll
             for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = pl[p];
+            }
         };
         auto eight = [&](const float *row, int i, float (&x)[8]) {
             if (i + 8 <= n_samples) {
@@ -613,12 +690,14 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
             }
         };
         auto fetch_weights = [&](int i0) {
-            if (MARKED) {
+            if constexpr (READY) {
+#pragma unroll
+                for (int p = 0; p < 3; ++p) w_ready[p] = f.wp[(group(i0, w_group) + p) * H + w_n];
+            } else if constexpr (MARKED) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    w[e] = w_row[(int64_t)__builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * w_group + e, n_samples - 1))) * H];
-                return;
-            }
+                    w[e] = (w_row + (int64_t)__builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * w_group + e, n_samples - 1))) * H)[w_n];
+            } else {
             eight(w_row, i0 + 8 * w_group, w);
             if (w_more)
                 for (int o = (n0 + w_col) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
@@ -629,8 +708,13 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
 #pragma unroll
                     for (int e = 0; e < 8; ++e) w[e] += y[e];
                 }
+            }
         };
         auto stage_weights = [&](int i0, int buf) {
+            if constexpr (READY) {
+#pragma unroll
+                for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col] = __builtin_bit_cast(uint4, w_ready[p]);
+            } else {
             float x[8];
             uint4 pl[3];
 #pragma unroll
@@ -641,6 +725,7 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
             split8(x, pl);
 #pragma unroll
             for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col] = pl[p];
+            }
         };
         __syncthreads();                               // the segment before is read
         if (of_ratios) fetch_ratios(0);
@@ -673,11 +758,14 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
             __syncthreads();
         }
     }
-    if (MARKED && I == 1 && sums) {                    // a part of the samples
+    };
+    if constexpr (MARKED) pass(std::true_type{});
+    pass(std::false_type{});
+    if (MARKED && I == 1 && f.sums) {                    // a part of the samples
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int64_t c = c0 + cw + 4 * half + 8 * (e / 4) + e % 4;
-            if (c < m.n_cats && n0 + nw + col < H) sums[(blockIdx.y * (int64_t)m.n_cats + c) * H + n0 + nw + col] = acc[0][0][e];
+            if (c < m.n_cats && n0 + nw + col < H) f.sums[(blockIdx.y * (int64_t)m.n_cats + c) * H + n0 + nw + col] = acc[0][0][e];
         }
         return;
     }
@@ -838,21 +926,27 @@ static int64_t flow_tiles(const pc_mixture &m, int64_t ic)
 // 512 states x 50257: B = 16 87 and 59, B = 94 124 and 106, B = 256 198 and 206, with 16 categories a sample 106 and 77).
 static bool flow_wide(const pc_mixture &m) { return flow_tiles(m, 2) >= 3000; }
 
-// Scratch of the flows: k_flow_prepare's wt, then (from byte `marks` on) its marks, then (from byte `sums` on) the sums of parts.  Preparing pays from some 64 samples on where tiles are
-// wide (4096 states x 50257, B = 64: 64 categories a sample 376 us against 447, gradients without zeros 447 against 450), from 128 where they are not
-// (512 states, B = 128: without zeros 126 against 116; B = 256 with 64 categories a sample 81 against 176).
+// Scratch of the flows: what k_flow_prepare makes, where it begins, then the sums of parts.  Preparing pays from some 32 samples on (4096 states
+// x 50257, B = 40: 64 categories a sample 372 us against 417, gradients without zeros 398 against 419; 512 states x 50257, B = 77: 72 against 96
+// and 91 against 98), where there is little to do from 128 (128 states x 256, B = 100: 25 against 18).
 // Where 64 x 64 tiles are few the samples are dealt out to several workgroups a tile, `part` each (a multiple of 64), whose sums k_flow_join
 // adds up, always in the same order (128 states x 256, B = 512 28 us against 53; 512 states x 4000, B = 256 in 1000 workgroups 39 against 30).
 constexpr int64_t kFlowGroups = 512, kFlowParts = 64;
-struct FlowSpace { size_t marks, sums, bytes; int32_t part, parts; };
+struct FlowSpace { size_t marks, wp, rp, sums, bytes; int32_t part, parts; };
 static FlowSpace flow_space(const pc_mixture &m, int32_t B)
 {
-    if (B < (flow_wide(m) ? 64 : 128)) return {0, 0, 0, B, 1};
+    if (B < (flow_tiles(m, 1) >= 2048 ? 32 : 128)) return {0, 0, 0, 0, 0, B, 1};
     const int64_t H = (int64_t)m.n_blocks * m.K, tiles = (m.n_cats + 63ll) / 64 * ((H + 63) / 64);
     const int64_t want = std::max<int64_t>(1, std::min(kFlowGroups / tiles, kFlowParts));
     const int32_t part = (int32_t)(((B + want - 1) / want + 63) / 64 * 64), parts = (B + part - 1) / part;
-    const size_t marks = ((size_t)B * H * 4 + 15) / 16 * 16, sums = marks + ((size_t)((m.n_cats + 63ll) / 64 * ((B + 31ll) / 32)) * 4 + 15) / 16 * 16;
-    return {marks, sums, sums + (parts > 1 ? (size_t)parts * m.n_cats * H * 4 : 0), part, parts};
+    const size_t groups = (B + 15ull) / 16 * 2;
+    FlowSpace f{0, 0, 0, 0, 0, part, parts};
+    f.marks = ((size_t)B * H * 4 + 15) / 16 * 16;
+    f.wp = f.marks + ((size_t)((m.n_cats + 63ll) / 64 * ((B + 31ll) / 32)) * 4 + 15) / 16 * 16;
+    f.rp = f.wp + groups * 3 * H * 16;
+    f.sums = f.rp + groups * 3 * m.n_cats * 16;
+    f.bytes = f.sums + (parts > 1 ? (size_t)parts * m.n_cats * H * 4 : 0);
+    return f;
 }
 
 static pc_status check_mixture(const pc_mixture *m, int32_t B)
@@ -938,18 +1032,18 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     const FlowSpace f = flow_space(*m, B);
     if (workspace_bytes < f.bytes) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_backward_workspace_bytes");
     if (f.bytes && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
-    float *wt = (float *)workspace;
-    uint32_t *marks = (uint32_t *)((char *)workspace + f.marks);
-    float *sums = f.parts > 1 ? (float *)((char *)workspace + f.sums) : nullptr;
+    char *base = (char *)workspace;
+    const FlowPrep prep{(float *)base, (uint32_t *)(base + f.marks), (pc_u32x4 *)(base + f.wp), (pc_u32x4 *)(base + f.rp), f.parts > 1 ? (float *)(base + f.sums) : nullptr, f.part};
+    const bool wide = flow_wide(*m);
     if (f.bytes) {
-        const int64_t turns = (H + 63) / 64 * ((B + 63ll) / 64), jobs = (m->n_cats + 63ll) / 64 * ((B + 31ll) / 32);
-        if (turns + jobs / 4 >= 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of weights and gradients");
-        hipLaunchKernelGGL(k_flow_prepare, dim3((unsigned)(turns + (jobs + 3) / 4)), dim3(256), 0, s, *m, B, dlogp, dlogp_ld, (int32_t)turns, wt, marks);
+        const int64_t I = wide ? 2 : 1, turns = (H + 63) / 64 * ((B + 63ll) / 64), segments = (f.part + kSegment - 1) / kSegment;
+        const int64_t jobs = (m->n_cats + 64 * I - 1) / (64 * I) * f.parts * segments;
+        if (turns + jobs >= 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of weights and gradients");
+        hipLaunchKernelGGL((wide ? k_flow_prepare<2> : k_flow_prepare<1>), dim3((unsigned)(turns + jobs)), dim3(64 * kPrepareWaves), 0, s, *m, B, logp, logp_ld, dlogp, dlogp_ld, (int32_t)turns, prep);
     }
 #define PC_FLOW(I, MARKED, LISTS)                                                                                                       \
     hipLaunchKernelGGL((k_predict_flow<I, MARKED, LISTS>), dim3((unsigned)flow_tiles(*m, I), f.parts), dim3(256), 0, s, *m, tables, B, logp, logp_ld, \
-                       dlogp, dlogp_ld, scale, accumulate, table_flow, wt, marks, f.part, sums)
-    const bool wide = flow_wide(*m);
+                       dlogp, dlogp_ld, scale, accumulate, table_flow, prep)
     if (f.bytes && wide) PC_FLOW(2, true, false);
     else if (f.bytes) PC_FLOW(1, true, false);
     else if (m->table && wide) PC_FLOW(2, false, true);
@@ -957,8 +1051,8 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     else if (wide) PC_FLOW(2, false, false);
     else PC_FLOW(1, false, false);
 #undef PC_FLOW
-    if (sums)
-        hipLaunchKernelGGL(k_flow_join, dim3((unsigned)((H + 63) / 64), (unsigned)((m->n_cats + 15ll) / 16)), dim3(256), 0, s, *m, tables, sums, f.parts, scale, accumulate, table_flow);
+    if (prep.sums)
+        hipLaunchKernelGGL(k_flow_join, dim3((unsigned)((H + 63) / 64), (unsigned)((m->n_cats + 15ll) / 16)), dim3(256), 0, s, *m, tables, prep.sums, f.parts, scale, accumulate, table_flow);
     return launched();
 }
 

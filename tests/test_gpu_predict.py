@@ -71,7 +71,7 @@ SIZES = [(1, 1, 1, 1), (1, 3, 2, 5), (2, 1, 7, 33), (7, 5, 65, 31), (16, 1, 64, 
          # blocks that are no multiple of four states: each remainder, few samples and many, the shortest blocks of the matrix cores
          (4, 9, 100, 40), (5, 7, 33000, 1), (6, 300, 60, 200), (7, 600, 5000, 33), (9, 5, 33000, 2), (127, 3, 8200, 300), (33, 69, 582, 460), (3, 40, 90, 70),
          # states dealt out to several workgroups: a short last part, one sample, every width of a wave
-         (128, 8, 40, 1), (20, 53, 300, 37), (32, 37, 700, 65), (128, 9, 5001, 129), (100, 13, 130, 300), (64, 18, 20000, 33)]
+         (128, 8, 40, 1), (20, 53, 300, 37), (32, 37, 700, 65), (128, 9, 5001, 129), (100, 13, 130, 300), (64, 18, 20000, 33), (128, 16, 33000, 21), (64, 4, 40000, 45), (96, 9, 30001, 31)]
 
 
 @pytest.mark.parametrize("K,nb,V,B", SIZES)
@@ -127,7 +127,7 @@ def test_block_lists_with_gaps_shared_tables_and_entries_out_of_range():
         check_flow(got[j], (ws @ r).T * t[j], (ws @ np.abs(r)).T * t[j], B * len(mine))
 
 
-@pytest.mark.parametrize("B,density", [(64, 0.004), (127, 0.02), (128, 0.0), (130, 0.002), (300, 0.01), (700, 0.002), (1100, 0.02), (256, 0.9)])
+@pytest.mark.parametrize("B,density", [(20, 0.3), (31, 0.004), (32, 0.004), (64, 0.004), (127, 0.02), (128, 0.0), (130, 0.002), (300, 0.01), (700, 0.002), (1100, 0.02), (256, 0.9)])
 @pytest.mark.parametrize("shared", [False, True])
 @pytest.mark.parametrize("V", [16500, 1001])
 def test_flows_of_targets_of_few_categories(B, density, shared, V):
