@@ -619,145 +619,145 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
     bool none = true;                                  // no sample counts for this tile
     // READY: the segments whose operands are as k_flow_prepare has left them; else the others.  Each way has its own loop: its registers are its own.
     auto pass = [&](auto as_ready) {
-    constexpr bool READY = decltype(as_ready)::value;
-    for (int s0 = first; s0 < last; s0 += MARKED ? kSegment : B) {
-        const int here = MARKED ? min(kSegment, last - s0) : B;
-        int n_samples = here;
-        if (MARKED) {
-            // lane i has the marks of samples 32 i to 32 i + 31; the list is made of them in order
-            const uint32_t word = s0 == first ? first_word : marks_of(s0, here);
-            int n = 0;
+        constexpr bool READY = decltype(as_ready)::value;
+        for (int s0 = first; s0 < last; s0 += MARKED ? kSegment : B) {
+            const int here = MARKED ? min(kSegment, last - s0) : B;
+            int n_samples = here;
+            if (MARKED) {
+                // lane i has the marks of samples 32 i to 32 i + 31; the list is made of them in order
+                const uint32_t word = s0 == first ? first_word : marks_of(s0, here);
+                int n = 0;
 #pragma unroll
-            for (int j = 0; j < kSegment / 32; ++j) n += __popc(__builtin_amdgcn_readlane(word, j));
-            if (mostly(n, here) != READY || n == 0) continue;
-            if (!READY) {
-                n_samples = n;
-                __syncthreads();                       // the list before is read
-                if (wave == 0)
-                    for (int j = 0, at = 0; j < (here + 31) / 32; ++j) {
-                        const uint32_t those = __builtin_amdgcn_readlane(word, j);
-                        if (lane < 32 && those >> lane & 1) list[at + __popc(those & ((1u << lane) - 1))] = (uint16_t)(32 * j + lane);
-                        at += __popc(those);
+                for (int j = 0; j < kSegment / 32; ++j) n += __popc(__builtin_amdgcn_readlane(word, j));
+                if (mostly(n, here) != READY || n == 0) continue;
+                if (!READY) {
+                    n_samples = n;
+                    __syncthreads();                       // the list before is read
+                    if (wave == 0)
+                        for (int j = 0, at = 0; j < (here + 31) / 32; ++j) {
+                            const uint32_t those = __builtin_amdgcn_readlane(word, j);
+                            if (lane < 32 && those >> lane & 1) list[at + __popc(those & ((1u << lane) - 1))] = (uint16_t)(32 * j + lane);
+                            at += __popc(those);
+                        }
+                    __syncthreads();
+                }
+            }
+            none = false;
+            int cat = (int)min(c0 + r_cat, (int64_t)m.n_cats - 1), w_n = min(n0 + w_col, H - 1);
+            if (MARKED) asm volatile("" : "+v"(cat), "+v"(w_n));     // addresses are made here, not kept for both ways
+            auto sample = [&](int i) { return s0 + (!MARKED ? i : list[i]); };
+            float l[READY ? 1 : 8], d[READY ? 1 : 8], w[READY ? 1 : 8];
+            pc_u32x4 r_ready[3], w_ready[3];
+            auto group = [&](int i, int which) { return (int64_t)min((s0 + i) / 8 + which, (B + 15) / 16 * 2 - 1) * 3; };
+            auto fetch_ratios = [&](int i0) {
+                if constexpr (READY) {
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) r_ready[p] = f.rp[(group(i0, r_group) + p) * m.n_cats + cat];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int64_t at = __builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * r_group + e, n_samples - 1)));
+                        l[e] = (logp + at * lp_ld)[cat];
+                        d[e] = (dlogp + at * dl_ld)[cat];
                     }
+                }
+            };
+            auto stage_ratios = [&](int i0, int buf) {
+                if constexpr (READY) {
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = __builtin_bit_cast(uint4, r_ready[p]);
+                } else {
+                    float x[8];
+                    uint4 pl[3];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = flow_ratio(l[e], d[e]);
+                    if (i0 + 16 > n_samples)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = i0 + 8 * r_group + e < n_samples ? x[e] : 0.0f;
+                    split8(x, pl);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = pl[p];
+                }
+            };
+            auto eight = [&](const float *row, int i, float (&x)[8]) {
+                if (i + 8 <= n_samples) {
+                    const Pack<float> u = load_pack(row + i), v = load_pack(row + i + 4);      // a row may begin at any float
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { x[e] = u.v[e]; x[4 + e] = v.v[e]; }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = row[min(i + e, n_samples - 1)];
+                }
+            };
+            auto fetch_weights = [&](int i0) {
+                if constexpr (READY) {
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) w_ready[p] = f.wp[(group(i0, w_group) + p) * H + w_n];
+                } else if constexpr (MARKED) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        w[e] = (w_row + (int64_t)__builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * w_group + e, n_samples - 1))) * H)[w_n];
+                } else {
+                    eight(w_row, i0 + 8 * w_group, w);
+                    if (w_more)
+                        for (int o = (n0 + w_col) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
+                            const MixBlock blk = mix_block(m, o);
+                            if (blk.row < 0 || blk.table != t) continue;
+                            float y[8];
+                            eight(m.weights + (blk.row + (n0 + w_col) % m.K) * m.stride, i0 + 8 * w_group, y);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) w[e] += y[e];
+                        }
+                }
+            };
+            auto stage_weights = [&](int i0, int buf) {
+                if constexpr (READY) {
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col] = __builtin_bit_cast(uint4, w_ready[p]);
+                } else {
+                    float x[8];
+                    uint4 pl[3];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = w[e] * kUp;
+                    if (i0 + 16 > n_samples)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = i0 + 8 * w_group + e < n_samples ? x[e] : 0.0f;
+                    split8(x, pl);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col] = pl[p];
+                }
+            };
+            __syncthreads();                               // the segment before is read
+            if (of_ratios) fetch_ratios(0);
+            if (of_weights) fetch_weights(0);
+            if (of_ratios) { stage_ratios(0, 0); fetch_ratios(16); }
+            if (of_weights) { stage_weights(0, 0); fetch_weights(16); }
+            __syncthreads();
+            for (int i0 = 0, buf = 0; i0 < n_samples; i0 += 16, buf ^= 1) {
+                const bool next = i0 + 16 < n_samples;
+                uint4 rp[I][3];
+#pragma unroll
+                for (int i = 0; i < I; ++i)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) rp[i][p] = rs[buf][p][half][cw + 32 * i + col];
+#pragma unroll
+                for (int k = 0; k < I; ++k) {
+                    uint4 wp[3];
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) wp[p] = ws[buf][p][half][nw + 32 * k + col];
+#pragma unroll
+                    for (int sum = 2; sum >= 0; --sum)     // the small products first
+#pragma unroll
+                        for (int p = sum; p >= 0; --p)
+#pragma unroll
+                            for (int i = 0; i < I; ++i) acc[i][k] = mfma(rp[i][p], wp[sum - p], acc[i][k]);
+                    if (next && k == 0 && of_weights) { stage_weights(i0 + 16, buf ^ 1); fetch_weights(i0 + 32); }
+                    if (next && k == I - 1 && of_ratios) { stage_ratios(i0 + 16, buf ^ 1); fetch_ratios(i0 + 32); }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
                 __syncthreads();
             }
         }
-        none = false;
-        int cat = (int)min(c0 + r_cat, (int64_t)m.n_cats - 1), w_n = min(n0 + w_col, H - 1);
-        if (MARKED) asm volatile("" : "+v"(cat), "+v"(w_n));     // addresses are made here, not kept for both ways
-        auto sample = [&](int i) { return s0 + (!MARKED ? i : list[i]); };
-        float l[READY ? 1 : 8], d[READY ? 1 : 8], w[READY ? 1 : 8];
-        pc_u32x4 r_ready[3], w_ready[3];
-        auto group = [&](int i, int which) { return (int64_t)min((s0 + i) / 8 + which, (B + 15) / 16 * 2 - 1) * 3; };
-        auto fetch_ratios = [&](int i0) {
-            if constexpr (READY) {
-#pragma unroll
-                for (int p = 0; p < 3; ++p) r_ready[p] = f.rp[(group(i0, r_group) + p) * m.n_cats + cat];
-            } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int64_t at = __builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * r_group + e, n_samples - 1)));
-                l[e] = (logp + at * lp_ld)[cat];
-                d[e] = (dlogp + at * dl_ld)[cat];
-            }
-            }
-        };
-        auto stage_ratios = [&](int i0, int buf) {
-            if constexpr (READY) {
-#pragma unroll
-                for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = __builtin_bit_cast(uint4, r_ready[p]);
-            } else {
-            float x[8];
-            uint4 pl[3];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = flow_ratio(l[e], d[e]);
-            if (i0 + 16 > n_samples)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = i0 + 8 * r_group + e < n_samples ? x[e] : 0.0f;
-            split8(x, pl);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) rs[buf][p][r_group][r_cat] = pl[p];
-            }
-        };
-        auto eight = [&](const float *row, int i, float (&x)[8]) {
-            if (i + 8 <= n_samples) {
-                const Pack<float> u = load_pack(row + i), v = load_pack(row + i + 4);      // a row may begin at any float
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { x[e] = u.v[e]; x[4 + e] = v.v[e]; }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = row[min(i + e, n_samples - 1)];
-            }
-        };
-        auto fetch_weights = [&](int i0) {
-            if constexpr (READY) {
-#pragma unroll
-                for (int p = 0; p < 3; ++p) w_ready[p] = f.wp[(group(i0, w_group) + p) * H + w_n];
-            } else if constexpr (MARKED) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    w[e] = (w_row + (int64_t)__builtin_amdgcn_readfirstlane(sample(min(i0 + 8 * w_group + e, n_samples - 1))) * H)[w_n];
-            } else {
-            eight(w_row, i0 + 8 * w_group, w);
-            if (w_more)
-                for (int o = (n0 + w_col) / m.K + 1, t = m.table[o - 1]; o < m.n_blocks; ++o) {
-                    const MixBlock blk = mix_block(m, o);
-                    if (blk.row < 0 || blk.table != t) continue;
-                    float y[8];
-                    eight(m.weights + (blk.row + (n0 + w_col) % m.K) * m.stride, i0 + 8 * w_group, y);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] += y[e];
-                }
-            }
-        };
-        auto stage_weights = [&](int i0, int buf) {
-            if constexpr (READY) {
-#pragma unroll
-                for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col] = __builtin_bit_cast(uint4, w_ready[p]);
-            } else {
-            float x[8];
-            uint4 pl[3];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = w[e] * kUp;
-            if (i0 + 16 > n_samples)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = i0 + 8 * w_group + e < n_samples ? x[e] : 0.0f;
-            split8(x, pl);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) ws[buf][p][w_group][w_col] = pl[p];
-            }
-        };
-        __syncthreads();                               // the segment before is read
-        if (of_ratios) fetch_ratios(0);
-        if (of_weights) fetch_weights(0);
-        if (of_ratios) { stage_ratios(0, 0); fetch_ratios(16); }
-        if (of_weights) { stage_weights(0, 0); fetch_weights(16); }
-        __syncthreads();
-        for (int i0 = 0, buf = 0; i0 < n_samples; i0 += 16, buf ^= 1) {
-            const bool next = i0 + 16 < n_samples;
-            uint4 rp[I][3];
-#pragma unroll
-            for (int i = 0; i < I; ++i)
-#pragma unroll
-                for (int p = 0; p < 3; ++p) rp[i][p] = rs[buf][p][half][cw + 32 * i + col];
-#pragma unroll
-            for (int k = 0; k < I; ++k) {
-                uint4 wp[3];
-#pragma unroll
-                for (int p = 0; p < 3; ++p) wp[p] = ws[buf][p][half][nw + 32 * k + col];
-#pragma unroll
-                for (int sum = 2; sum >= 0; --sum)     // the small products first
-#pragma unroll
-                    for (int p = sum; p >= 0; --p)
-#pragma unroll
-                        for (int i = 0; i < I; ++i) acc[i][k] = mfma(rp[i][p], wp[sum - p], acc[i][k]);
-                if (next && k == 0 && of_weights) { stage_weights(i0 + 16, buf ^ 1); fetch_weights(i0 + 32); }
-                if (next && k == I - 1 && of_ratios) { stage_ratios(i0 + 16, buf ^ 1); fetch_ratios(i0 + 32); }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            __syncthreads();
-        }
-    }
     };
     if constexpr (MARKED) pass(std::true_type{});
     pass(std::false_type{});
