@@ -354,59 +354,51 @@ __global__ __launch_bounds__(256) void k_predict_join(const float *__restrict__ 
     logp[i / n_cats * ld + i % n_cats] = log_p(p);
 }
 
-// A few samples: bound by reading the tables once.  The lanes of a wave cover whole table rows (K / 4 lanes each with four states) of the
-// same block, so that loads are contiguous, kFewRows of two blocks in flight; a lane keeps its states' weights of the block in registers
-// and a sum per row and sample, and only at the end of all blocks the lanes of a row add theirs.  Products in fp32.
-constexpr int kFewFloats = 4096, kFewRows = 8;         // weights in LDS at a time; loads of a lane in flight, of two blocks each
-template <int NS>
-__global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const float *__restrict__ tables, int32_t B, float *__restrict__ logp, int64_t ld)
+// One sample: bound by reading the tables once.  The lanes of a wave cover whole table rows (K / 4 lanes each with four states) of the
+// same block, so that loads are contiguous, kOneRows of two blocks in flight; a lane keeps its states' weights of the block in registers
+// and a sum per row, and only at the end of all blocks the lanes of a row add theirs.  Products in fp32.
+constexpr int kOneFloats = 4096, kOneRows = 8;         // weights in LDS at a time; loads of a lane in flight, of two blocks each
+__global__ __launch_bounds__(256) void k_predict_one(const pc_mixture m, const float *__restrict__ tables, float *__restrict__ logp)
 {
-    __shared__ float4 w[kFewFloats / 4];              // [block of the window][sample][piece]
+    __shared__ float4 w[kOneFloats / 4];              // [block of the window][piece]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int P = group_states(m.K) / 4, R = 64 / P, piece = lane % P, r = lane / P;      // pieces of a row, rows of an instruction
     const bool idle = r >= R;
-    const int per_window = min(m.n_blocks, kFewFloats / (NS * 4 * P));      // at least 16: K <= 128, NS <= 2
-    const int64_t c0 = ((int64_t)blockIdx.x * 4 + wave) * R * kFewRows + (idle ? 0 : r);
-    float acc[kFewRows][NS];
+    const int per_window = min(m.n_blocks, kOneFloats / (4 * P));
+    const int64_t c0 = ((int64_t)blockIdx.x * 4 + wave) * R * kOneRows + (idle ? 0 : r);
+    float acc[kOneRows] = {};
     bool on[2];
+    int64_t row[kOneRows];                                 // a category behind the last reads that one's row again
 #pragma unroll
-    for (int u = 0; u < kFewRows; ++u)
-#pragma unroll
-        for (int s = 0; s < NS; ++s) acc[u][s] = 0.0f;
-    int64_t row[kFewRows];                                 // a category behind the last reads that one's row again
-#pragma unroll
-    for (int u = 0; u < kFewRows; ++u) row[u] = min(c0 + u * R, (int64_t)m.n_cats - 1) * m.K + group_start(m.K, 4 * piece);
+    for (int u = 0; u < kOneRows; ++u) row[u] = min(c0 + u * R, (int64_t)m.n_cats - 1) * m.K + group_start(m.K, 4 * piece);
     for (int j0 = 0; j0 < m.n_blocks; j0 += per_window) {
         const int here = min(per_window, m.n_blocks - j0);
         __syncthreads();
-        for (int i = threadIdx.x; i < here * P * NS; i += 256) {
-            const int b = i % NS, q = i / NS % P, j = i / (NS * P);
-            const MixBlock blk = mix_block(m, j0 + j);
+        for (int i = threadIdx.x; i < here * P; i += 256) {
+            const int q = i % P;
+            const MixBlock blk = mix_block(m, j0 + i / P);
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (blk.row >= 0 && b < B) {
+            if (blk.row >= 0) {
                 const int k = group_start(m.K, 4 * q), skip = 4 * q - k;
-                const float *src = m.weights + (blk.row + k) * m.stride + b;
+                const float *src = m.weights + (blk.row + k) * m.stride;
                 v = make_float4(skip > 0 ? 0.f : src[0], skip > 1 ? 0.f : src[m.stride], skip > 2 ? 0.f : src[2 * m.stride], src[3 * m.stride]);
             }
-            w[(j * NS + b) * P + q] = v;
+            w[i] = v;
         }
         __syncthreads();
-        Pack<float> t[2][kFewRows];                             // a block's rows, while those of the one before are added up
+        Pack<float> t[2][kOneRows];                             // a block's rows, while those of the one before are added up
         auto fetch = [&](int j, int set) {             // a block left out reads the first table's rows and is not added
             const MixBlock blk = mix_block(m, j0 + j);
             on[set] = blk.row >= 0;
             const float *src = tables + (int64_t)max(blk.table, 0) * m.n_cats * m.K;
 #pragma unroll
-            for (int u = 0; u < kFewRows; ++u) t[set][u] = load_pack(src + row[u]);
+            for (int u = 0; u < kOneRows; ++u) t[set][u] = load_pack(src + row[u]);
         };
         auto add = [&](int j, int set) {
             if (!on[set]) return;
+            const float4 v = w[j * P + piece];
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const float4 v = w[(j * NS + s) * P + piece];
-#pragma unroll
-                for (int u = 0; u < kFewRows; ++u) acc[u][s] += t[set][u].v[0] * v.x + t[set][u].v[1] * v.y + t[set][u].v[2] * v.z + t[set][u].v[3] * v.w;
-            }
+            for (int u = 0; u < kOneRows; ++u) acc[u] += t[set][u].v[0] * v.x + t[set][u].v[1] * v.y + t[set][u].v[2] * v.z + t[set][u].v[3] * v.w;
         };
         fetch(0, 0);
         for (int j = 0; j < here; j += 2) {
@@ -419,17 +411,14 @@ __global__ __launch_bounds__(256) void k_predict_few(const pc_mixture m, const f
         }
     }
 #pragma unroll
-    for (int u = 0; u < kFewRows; ++u) {
+    for (int u = 0; u < kOneRows; ++u) {
         const int64_t c = c0 + u * R;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            float v = acc[u][s];
-            for (int d = 1; d < P; d <<= 1) {          // lane `piece` adds d lanes more each time, none of another row
-                const float o = __shfl_down(v, d);
-                if (piece + d < P && piece % (2 * d) == 0) v += o;
-            }
-            if (piece == 0 && !idle && s < B && c < m.n_cats) logp[s * ld + c] = log_p(v);
+        float v = acc[u];
+        for (int d = 1; d < P; d <<= 1) {              // lane `piece` adds d lanes more each time, none of another row
+            const float o = __shfl_down(v, d);
+            if (piece + d < P && piece % (2 * d) == 0) v += o;
         }
+        if (piece == 0 && !idle && c < m.n_cats) logp[c] = log_p(v);
     }
 }
 
@@ -844,11 +833,11 @@ __global__ __launch_bounds__(256) void k_flow_join(const pc_mixture m, const flo
     }
 }
 
-static int64_t few_rows(const pc_mixture &m) { return 64 / ((m.K + 3) / 4) * kFewRows; }      // categories of a wave of k_predict_few
+static int64_t one_rows(const pc_mixture &m) { return 64 / ((m.K + 3) / 4) * kOneRows; }      // categories of a wave of k_predict_one
 
 // How a prediction is launched.
-// One or two samples of many categories: no matrix cores (4096 states x 50257 at one sample: 168 us against 211 with them, at four 163 with them
-// against 200), where that makes waves enough for two to a CU.
+// One sample of many categories: no matrix cores (100 states x 20 blocks x 50257 80 us against 101, 32 states x 8 14 against 18; 4096 states 156 and
+// 154, 8192 states x 20000 133 and 119; two samples of 4096 163 and 156), where that makes waves enough for two to a CU.
 // Two planes an operand where log-probabilities are large (many categories), three where they are not: an error of 2^-18 of a probability
 // is 10^-6 of a logarithm of -4, but as much as the logarithm's own rounding allows at -10.
 // Samples a wave: as many of 256 as there are, so that the tables are read once; fewer where that leaves a SIMD without a wave (the
@@ -856,13 +845,13 @@ static int64_t few_rows(const pc_mixture &m) { return 64 / ((m.K + 3) / 4) * kFe
 // Where there is less than a workgroup to a CU and the states are many (1024: an exchange and a second launch take some 4 us) they are dealt out
 // in parts of at least 256, as many as fill the GPU once, whose sums k_predict_join adds up (4096 states x 256, B = 256 22 us against 61;
 // x 5000 63 against 144; x 16000, 2048 states, B = 500 124 against 135; with more workgroups, 1024 states x 50257, B = 64 66 against 49).
-struct PredictPlan { bool few, exact; int32_t nt, len, parts, columns; size_t sums, bytes; };
+struct PredictPlan { bool one, exact; int32_t nt, len, parts, columns; size_t sums, bytes; };
 static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
 {
     PredictPlan p{};
     if (m.K < 4) return p;
-    p.few = B <= 2 && m.n_cats >= 512 * few_rows(m);
-    if (p.few) return p;
+    p.one = B == 1 && m.n_cats >= 512 * one_rows(m);
+    if (p.one) return p;
     const int64_t rows = (m.n_cats + 31ll) / 32, H = (int64_t)m.n_blocks * ((m.K + 3) / 4 * 4), most = H < 1024 ? 1 : H / 256;
     p.exact = m.n_cats < 4096;
     p.nt = B > 128 && !p.exact ? 8 : B > 64 ? 4 : B > 32 ? 2 : 1;
@@ -879,12 +868,19 @@ static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
     return p;
 }
 
+// Samples of a first launch with the widest waves, the others in a second one: where half of such a wave would do for those (4096 states
+// x 50257, B = 257 490 us against 602).
+static int32_t predict_first(const pc_mixture &m, int32_t B)
+{
+    if (B <= 256 || B % 256 == 0 || B % 256 > 128) return B;
+    const PredictPlan p = predict_plan(m, B);
+    return p.nt == 8 && p.parts == 1 ? B / 256 * 256 : B;
+}
+
 static void launch_predict(const pc_mixture &m, const PredictPlan &p, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace, hipStream_t s)
 {
-    if (p.few) {
-        const dim3 grid((unsigned)((m.n_cats + 4 * few_rows(m) - 1) / (4 * few_rows(m))));
-        if (B == 1) hipLaunchKernelGGL((k_predict_few<1>), grid, dim3(256), 0, s, m, tables, B, logp, ld);
-        else hipLaunchKernelGGL((k_predict_few<2>), grid, dim3(256), 0, s, m, tables, B, logp, ld);
+    if (p.one) {
+        hipLaunchKernelGGL(k_predict_one, dim3((unsigned)((m.n_cats + 4 * one_rows(m) - 1) / (4 * one_rows(m)))), dim3(256), 0, s, m, tables, logp);
         return;
     }
     const int64_t rows = (m.n_cats + 31ll) / 32;
@@ -979,7 +975,8 @@ pc_status pc_predict_workspace_bytes(const pc_mixture *m, int32_t B, size_t *byt
     const pc_status st = check_mixture(m, B);
     if (st != PC_OK) return st;
     if (!bytes) return fail(PC_ERR_ARG, "NULL argument");
-    *bytes = predict_plan(*m, B).bytes;
+    const int32_t first = predict_first(*m, B);
+    *bytes = std::max(predict_plan(*m, first).bytes, first < B ? predict_plan(*m, B - first).bytes : 0);
     return PC_OK;
 }
 
@@ -996,10 +993,17 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
         hipLaunchKernelGGL(k_predict_any, grid, dim3(256), 0, (hipStream_t)stream, *m, tables, B, logp, ld);
         return launched();
     }
-    const PredictPlan p = predict_plan(*m, B);
-    if (workspace_bytes < p.bytes) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_workspace_bytes");
-    if (p.bytes && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
-    launch_predict(*m, p, tables, B, logp, ld, workspace, (hipStream_t)stream);
+    size_t need = 0;
+    pc_predict_workspace_bytes(m, B, &need);
+    if (workspace_bytes < need) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_workspace_bytes");
+    if (need && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
+    const int32_t first = predict_first(*m, B);
+    launch_predict(*m, predict_plan(*m, first), tables, first, logp, ld, workspace, (hipStream_t)stream);
+    if (first < B) {
+        pc_mixture rest = *m;
+        rest.weights += first;
+        launch_predict(rest, predict_plan(rest, B - first), tables, B - first, logp + first * ld, ld, workspace, (hipStream_t)stream);
+    }
     return launched();
 }
 
@@ -1023,9 +1027,6 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     if (logp_ld < m->n_cats || dlogp_ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4) || !aligned_to(dlogp, 4)) return fail(PC_ERR_ARG, "logp and dlogp must be 4-byte aligned");
     if (!aligned_to(table_flow, 16)) return fail(PC_ERR_ARG, "table_flow must be 16-byte aligned");
-    // Tiles: of very many, 128 x 256 from 128 samples on and 128 x 128 below (4096 states x 50257: B = 32 393 us against 466, B = 256 1161 against
-    // 981; by 64 x 64 412 at B = 32); of fewer, which such tiles would cover in two or three rounds of workgroups, 64 x 64 (512 states: B = 16
-    // 58 us against 86, B = 96 97 against 112).  Looking for samples to leave out pays from some 128 on.
     const int64_t H = (int64_t)m->n_blocks * m->K;
     const hipStream_t s = (hipStream_t)stream;
     if (flow_tiles(*m, 1) > 1 << 23) return fail(PC_ERR_TOO_LARGE, "more than 2^23 tiles of flows");

@@ -71,7 +71,9 @@ SIZES = [(1, 1, 1, 1), (1, 3, 2, 5), (2, 1, 7, 33), (7, 5, 65, 31), (16, 1, 64, 
          # blocks that are no multiple of four states: each remainder, few samples and many, the shortest blocks of the matrix cores
          (4, 9, 100, 40), (5, 7, 33000, 1), (6, 300, 60, 200), (7, 600, 5000, 33), (9, 5, 33000, 2), (127, 3, 8200, 300), (33, 69, 582, 460), (3, 40, 90, 70),
          # states dealt out to several workgroups: a short last part, one sample, every width of a wave
-         (128, 8, 40, 1), (20, 53, 300, 37), (32, 37, 700, 65), (128, 9, 5001, 129), (100, 13, 130, 300), (64, 18, 20000, 33), (128, 16, 33000, 21), (64, 4, 40000, 45), (96, 9, 30001, 31)]
+         (128, 8, 40, 1), (20, 53, 300, 37), (32, 37, 700, 65), (128, 9, 5001, 129), (100, 13, 130, 300), (64, 18, 20000, 33), (128, 16, 33000, 21), (64, 4, 40000, 45), (96, 9, 30001, 31),
+         # a batch in two launches
+         (36, 3, 33000, 257), (32, 2, 40001, 640)]
 
 
 @pytest.mark.parametrize("K,nb,V,B", SIZES)
