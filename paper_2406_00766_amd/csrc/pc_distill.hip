@@ -197,7 +197,7 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(co
 
 // Gradient.  The listed categories' values are made first (from the row itself where the gradient replaces it), then the dense part is
 // written in packs of the output's 16-byte grid, then, behind a barrier, the listed ones over it.  Bound by reading and writing (8192 x
-// 50257: fp32 718 us, 16 bits 358, 4.6 TB/s; a copy reaches 4.9).  Fetching the first packs before the list is made gained nothing.
+// 50257: fp32 625 us, 16 bits 325, 5.1 to 5.3 TB/s).  Fetching the first packs before the list is made gained nothing.
 template <typename TS, typename TT, int WAVES, bool LONG>
 __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(const DistillDev d, const float *__restrict__ stats,
                                                                                const float *__restrict__ dloss, float scale, void *dstudent, int64_t out_ld)
@@ -257,11 +257,18 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(co
         const TS *zg = z - off;                        // element i of the grid is category i - off
         TS *grid = out - off;
         const int64_t end = off + (int64_t)d.n_cats, p_first = off > 0, p_last = end / N;
+        // past the caches where sixteen waves hasten through a row: lines that wait there are written back after the last one (100 x 50257 fp32
+        // 12 us against 19, 8192 x 50257 bf16 325 against 331; with four waves 365 against 358)
+        auto put = [&](int64_t p, const Pack<TS> &v) {
+            pc_u32x4 *to = reinterpret_cast<pc_u32x4 *>(grid + p * N);
+            if (WAVES == 16) __builtin_nontemporal_store(__builtin_bit_cast(pc_u32x4, v), to);
+            else *to = __builtin_bit_cast(pc_u32x4, v);
+        };
         const int64_t edge = edge_of<N>(t, off, end);
         if (zeros) {
             if (edge >= 0) grid[edge] = from_f32<TS>(0.0f);
             const float x[N] = {};
-            for (int64_t p = p_first + t; p < p_last; p += TH) *reinterpret_cast<Pack<TS> *>(__builtin_assume_aligned(grid + p * N, 16)) = pack_f32<TS>(x);
+            for (int64_t p = p_first + t; p < p_last; p += TH) put(p, pack_f32<TS>(x));
         } else {
             if (edge >= 0) grid[edge] = from_f32<TS>(dense(to_f32(zg[edge])));
             auto step = [&](int64_t p0, auto some) {   // kPacks of which not all may be there
@@ -278,7 +285,7 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(co
                     unpack_f32(in[k], x);
 #pragma unroll
                     for (int e = 0; e < N; ++e) x[e] = dense(x[e]);
-                    if (!some || p < p_last) *reinterpret_cast<Pack<TS> *>(__builtin_assume_aligned(grid + p * N, 16)) = pack_f32<TS>(x);
+                    if (!some || p < p_last) put(p, pack_f32<TS>(x));
                 }
             };
             int64_t p0 = p_first;
@@ -321,15 +328,18 @@ static DistillDev distill_dev(const pc_distill *d)
 }
 // f(waves of a row, whether its list is long), as types: one wave where a row is at most 16 KB, four steps of a wave (one and four waves, us: loss of
 // 20000 x 1000 bf16 25 and 78, of 8192 x 4096 fp32 28 and 33, gradient 65 and 59; of 8192 x 8192 fp32 50 and 48); sixteen where rows are
-// fewer than `few`, else four (sixteen and four: loss of 100 x 50257 fp32 11.4 and 11.5, of 400 24 and 19, gradient of 100 19 and 23,
-// of 400 40 and 43, of 800 x 32000 bf16 33 and 29).
-constexpr int64_t kFewLoss = 128, kFewGrad = 512;
+// fewer than `few` or of `large` bytes, else four (sixteen and four: loss of 100 x 50257 fp32 11.4 and 11.5, of 400 24 and 19, gradient of 100
+// 12 and 23, of 400 39 and 43, of 800 x 32000 bf16 33 and 29; long rows are written faster when few of them are at work at a time: gradient of
+// 8192 x 50257 bf16 325 and 358, of 8192 x 32000 fp32 363 and 427, bf16 224 and 218).
+struct FewLong { int64_t few, large; };
+constexpr FewLong kLoss = {128, INT64_MAX}, kGrad = {512, 96 << 10};
 template <typename F>
-static void with_group(const pc_distill *d, int64_t few, F f)
+static void with_group(const pc_distill *d, FewLong rule, F f)
 {
+    const int64_t bytes = d->n_cats * type_bytes(d->student_type);
     if (d->top > kShortList) f(Group<4, true>{});
-    else if (d->n_cats * type_bytes(d->student_type) <= 16384) f(Group<1, false>{});
-    else if (d->rows < few) f(Group<16, false>{});
+    else if (bytes <= 16384) f(Group<1, false>{});
+    else if (d->rows < rule.few || bytes >= rule.large) f(Group<16, false>{});
     else f(Group<4, false>{});
 }
 template <typename G>
@@ -370,7 +380,7 @@ pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t worksp
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            with_group(d, kFewLoss, [&](auto g) {
+            with_group(d, kLoss, [&](auto g) {
                 using G = decltype(g);
                 hipLaunchKernelGGL((k_distill_rows<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
                                    (hipStream_t)stream, dev, loss, stats);
@@ -394,7 +404,7 @@ pc_status pc_distill_backward(const pc_distill *d, const float *stats, const flo
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            with_group(d, kFewGrad, [&](auto g) {
+            with_group(d, kGrad, [&](auto g) {
                 using G = decltype(g);
                 hipLaunchKernelGGL((k_distill_grad<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
                                    (hipStream_t)stream, dev, stats, dloss, scale, dstudent, dstudent_ld);
