@@ -239,15 +239,31 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(co
         const float f = g * (Q * expf(-log_s));
         auto dense = [&](float v) { return __builtin_amdgcn_exp2f((v - m) * c) * f; };
         if (listing && !none) {                        // a category listed more than once: its first entry writes for all
+            bool again = LONG;                         // a short list is looked through for such categories first (lists of 64, 8192 x 50257 bf16
+                                                       // 333 us against 373, 20000 x 1000 31 against 49; with doubled ones 55)
+            if (!LONG) {
+                const int32_t own = list.id[0] >= 0 ? list.id[0] : -1 - t;       // no two of those that are none are alike
+                uint64_t others = 0;
+#pragma unroll
+                for (int k = 0; k < 64; ++k) {
+                    if (k % 8 == 0 && k >= d.top) break;
+                    others |= __ballot(own == __builtin_amdgcn_readlane(own, k)) & ~(1ull << k);
+                }
+                again = others != 0;
+            }
 #pragma unroll
             for (int i = 0; i < G::LIST; ++i) {
                 const int j = t + i * TH;
                 bool first = list.id[i] >= 0;
-                float sum = 0.0f;
-                for (int k = 0; k < d.top; ++k) {
-                    const int32_t o = LONG ? ids[k] : __builtin_amdgcn_readlane(list.id[0], k);
-                    const float oq = LONG ? qs[k] : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.q[0]), k));
-                    if (o == list.id[i]) { first = first && k >= j; sum += oq; }
+                float sum = list.q[i];
+                if (again) {
+                    sum = 0.0f;
+#pragma unroll 4
+                    for (int k = 0; k < d.top; ++k) {
+                        const int32_t o = LONG ? ids[k] : __builtin_amdgcn_readlane(list.id[0], k);
+                        const float oq = LONG ? qs[k] : __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.q[0]), k));
+                        if (o == list.id[i]) { first = first && k >= j; sum += oq; }
+                    }
                 }
                 at[i] = (zeros ? 0.0f : dense(at[i])) - g * sum;
                 if (!first) list.id[i] = -1;
