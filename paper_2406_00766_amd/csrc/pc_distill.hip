@@ -25,11 +25,12 @@ struct DistillDev {                                   // pc_distill without its 
 
 __device__ inline float add2(float a, float b) { return a + b; }
 __device__ inline float max2(float a, float b) { return fmaxf(a, b); }
-// A row is worked on by WAVES waves of a workgroup.  Its list lies with the first of them where it has at most 64 entries (LONG = false: no
+// A row is worked on by WAVES waves of a workgroup; STREAM: rows that no cache holds until they are read again.  Its list lies with the first of them where it has at most 64 entries (LONG = false: no
 // barriers), else with all of them, LIST entries a lane.
 constexpr int kShortList = 64;
-template <int WAVES, bool LONG>
+template <int WAVES, bool LONG, bool STREAM = false>
 struct Group {
+    static constexpr bool STREAMS = STREAM;
     static constexpr int THREADS = 64 * WAVES, LIST = LONG ? PC_MAX_TOP / THREADS : 1;
     static constexpr int ROWS = WAVES >= 4 ? 1 : 4 / WAVES;              // rows of a workgroup
     static constexpr int BLOCK = THREADS * ROWS;
@@ -91,7 +92,7 @@ struct List {
 };
 
 // Loss and statistics.  A row passes through registers once, kPacks x 16 bytes a lane at a time, the next ones on their way, with a running
-// maximum and sum per lane: bound by reading it (8192 x 50257: fp32 270 us, 6.1 TB/s; 16 bits 147, 5.6 TB/s).  The list is made into
+// maximum and sum per lane: bound by reading it (8192 x 50257: fp32 247 us, 6.7 TB/s; 16 bits 137, 6.0 TB/s).  The list is made into
 // probabilities, and its student's logits are fetched, while the first packs are on their way.
 constexpr int kPacks = 4;
 // The element (of the grid that begins `off` elements before the row and has `end` up to the row's last) that lane t of a row takes of those
@@ -103,7 +104,7 @@ __device__ inline int64_t edge_of(int t, int off, int64_t end)
     if (t < N) return off > 0 && t >= off && t < end ? t : -1;
     return t < 2 * N && tail + t - N < end ? tail + t - N : -1;
 }
-template <typename TS, typename TT, int WAVES, bool LONG>
+template <typename TS, typename TT, int WAVES, bool LONG, bool STREAM>
 __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(const DistillDev d, float *__restrict__ loss, float *__restrict__ stats)
 {
     using G = Group<WAVES, LONG>;
@@ -134,7 +135,8 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(co
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k) {
                     const int64_t p = min(p0 + t + k * TH, p_last - 1);
-                    ahead[k] = load_pack((const TS *)__builtin_assume_aligned(grid + p * N, 16));
+                    const TS *from = (const TS *)__builtin_assume_aligned(grid + p * N, 16);
+                    ahead[k] = STREAM ? stream_pack(from) : load_pack(from);
                 }
             };
             if (p_first < p_last) fetch(p_first);
@@ -197,8 +199,8 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(co
 
 // Gradient.  The listed categories' values are made first (from the row itself where the gradient replaces it), then the dense part is
 // written in packs of the output's 16-byte grid, then, behind a barrier, the listed ones over it.  Bound by reading and writing (8192 x
-// 50257: fp32 625 us, 16 bits 325, 5.1 to 5.3 TB/s).  Fetching the first packs before the list is made gained nothing.
-template <typename TS, typename TT, int WAVES, bool LONG>
+// 50257: fp32 628 us, 16 bits 322, 5.1 to 5.2 TB/s).  Fetching the first packs before the list is made gained nothing.
+template <typename TS, typename TT, int WAVES, bool LONG, bool STREAM>
 __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(const DistillDev d, const float *__restrict__ stats,
                                                                                const float *__restrict__ dloss, float scale, void *dstudent, int64_t out_ld)
 {
@@ -292,7 +294,8 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_grad(co
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k) {
                     const int64_t p = p0 + t + k * TH;
-                    in[k] = load_pack(zg + (some ? min(p, p_last - 1) : p) * N);
+                    const TS *from = zg + (some ? min(p, p_last - 1) : p) * N;
+                    in[k] = STREAM ? stream_pack(from) : load_pack(from);
                 }
 #pragma unroll
                 for (int k = 0; k < kPacks; ++k) {
@@ -347,16 +350,26 @@ static DistillDev distill_dev(const pc_distill *d)
 // fewer than `few` or of `large` bytes, else four (sixteen and four: loss of 100 x 50257 fp32 11.4 and 11.5, of 400 24 and 19, gradient of 100
 // 12 and 23, of 400 39 and 43, of 800 x 32000 bf16 33 and 29; long rows are written faster when few of them are at work at a time: gradient of
 // 8192 x 50257 bf16 325 and 358, of 8192 x 32000 fp32 363 and 427, bf16 224 and 218).
-struct FewLong { int64_t few, large; };
-constexpr FewLong kLoss = {128, INT64_MAX}, kGrad = {512, 96 << 10};
-template <typename F>
-static void with_group(const pc_distill *d, FewLong rule, F f)
+// Rows of 256 MB and more together, which no cache holds until they are read again, are read past the caches by the widest waves that such
+// numbers come to: loss of 8192 x 50257 fp32 247 us against 272, 16 bits 137 and 148, gradient 628 and 637, 322 and 332; of 333 x 32003 fp16 18 and 15.
+struct RowRule { int64_t few, large; bool stream_four, stream_sixteen; };
+struct LossRule { static constexpr RowRule value = {128, INT64_MAX, true, false}; };
+struct GradRule { static constexpr RowRule value = {512, 96 << 10, false, true}; };
+template <typename Rule, typename F>
+static void with_group(const pc_distill *d, Rule, F f)
 {
+    constexpr RowRule rule = Rule::value;
     const int64_t bytes = d->n_cats * type_bytes(d->student_type);
+    const bool streams = d->rows * bytes >= 256 << 20;
     if (d->top > kShortList) f(Group<4, true>{});
     else if (bytes <= 16384) f(Group<1, false>{});
-    else if (d->rows < rule.few || bytes >= rule.large) f(Group<16, false>{});
-    else f(Group<4, false>{});
+    else if (d->rows < rule.few || bytes >= rule.large) {
+        if (rule.stream_sixteen && streams) f(Group<16, false, rule.stream_sixteen>{});
+        else f(Group<16, false>{});
+    } else {
+        if (rule.stream_four && streams) f(Group<4, false, rule.stream_four>{});
+        else f(Group<4, false>{});
+    }
 }
 template <typename G>
 static dim3 row_grid(int64_t rows) { return dim3((unsigned)std::min<int64_t>((rows + G::ROWS - 1) / G::ROWS, 1 << 20)); }
@@ -396,9 +409,9 @@ pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t worksp
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            with_group(d, kLoss, [&](auto g) {
+            with_group(d, LossRule{}, [&](auto g) {
                 using G = decltype(g);
-                hipLaunchKernelGGL((k_distill_rows<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
+                hipLaunchKernelGGL((k_distill_rows<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1), G::STREAMS>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
                                    (hipStream_t)stream, dev, loss, stats);
             });
         });
@@ -420,9 +433,9 @@ pc_status pc_distill_backward(const pc_distill *d, const float *stats, const flo
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {
-            with_group(d, kGrad, [&](auto g) {
+            with_group(d, GradRule{}, [&](auto g) {
                 using G = decltype(g);
-                hipLaunchKernelGGL((k_distill_grad<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1)>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
+                hipLaunchKernelGGL((k_distill_grad<decltype(s), decltype(t), G::THREADS / 64, (G::LIST > 1), G::STREAMS>), row_grid<G>(d->rows), dim3(G::BLOCK), 0,
                                    (hipStream_t)stream, dev, stats, dloss, scale, dstudent, dstudent_ld);
             });
         });

@@ -356,8 +356,10 @@ __global__ __launch_bounds__(256) void k_predict_join(const float *__restrict__ 
 
 // One sample: bound by reading the tables once.  The lanes of a wave cover whole table rows (K / 4 lanes each with four states) of the
 // same block, so that loads are contiguous, kOneRows of two blocks in flight; a lane keeps its states' weights of the block in registers
-// and a sum per row, and only at the end of all blocks the lanes of a row add theirs.  Products in fp32.
+// and a sum per row, and only at the end of all blocks the lanes of a row add theirs.  Products in fp32.  STREAM: tables of 256 MB and more,
+// which no cache holds until the next call, are read past the caches (4096 states x 50257 149 us against 162; 512 states, held, 23 against 22).
 constexpr int kOneFloats = 4096, kOneRows = 8;         // weights in LDS at a time; loads of a lane in flight, of two blocks each
+template <bool STREAM>
 __global__ __launch_bounds__(256) void k_predict_one(const pc_mixture m, const float *__restrict__ tables, float *__restrict__ logp)
 {
     __shared__ float4 w[kOneFloats / 4];              // [block of the window][piece]
@@ -392,7 +394,7 @@ __global__ __launch_bounds__(256) void k_predict_one(const pc_mixture m, const f
             on[set] = blk.row >= 0;
             const float *src = tables + (int64_t)max(blk.table, 0) * m.n_cats * m.K;
 #pragma unroll
-            for (int u = 0; u < kOneRows; ++u) t[set][u] = load_pack(src + row[u]);
+            for (int u = 0; u < kOneRows; ++u) t[set][u] = STREAM ? stream_pack(src + row[u]) : load_pack(src + row[u]);
         };
         auto add = [&](int j, int set) {
             if (!on[set]) return;
@@ -763,6 +765,7 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
     // before is stored.  Else entry by entry.
     auto finish = [&](auto add) {
         constexpr bool ADD = decltype(add)::value;
+        // (tables and flows past the caches, which keep the operands: B = 32 358 us against 383, 64 categories a sample, B = 256 420 against 446)
         float t[2][16];
         auto offset = [&](int sq) { return (uint32_t)((o_at[nw + 32 * (sq / I) + col] + (c0 + cw + 32 * (sq % I) + 4 * half) * m.K) * 4); };
         auto entry = [&](int e) { return (int64_t)(8 * (e / 4) + e % 4) * m.K * 4; };
@@ -770,7 +773,7 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
             const uint32_t at = offset(sq);
             if (MARKED && none) return;                  // the sums are zero
 #pragma unroll
-            for (int e = 0; e < 16; ++e) t[sq & 1][e] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(tables) + entry(e) + at);
+            for (int e = 0; e < 16; ++e) t[sq & 1][e] = __builtin_nontemporal_load(reinterpret_cast<const float *>(reinterpret_cast<const char *>(tables) + entry(e) + at));
         };
         fetch(0);
 #pragma unroll
@@ -785,7 +788,7 @@ __global__ __launch_bounds__(256, I == 2 ? 3 : 4) void k_predict_flow(const pc_m
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float v = MARKED && none ? 0.0f : scale * (t[sq & 1][e] * acc[sq % I][sq / I][e]);
-                    *reinterpret_cast<float *>(reinterpret_cast<char *>(flow) + entry(e) + at) = ADD ? old[e] + v : v;
+                    __builtin_nontemporal_store(ADD ? old[e] + v : v, reinterpret_cast<float *>(reinterpret_cast<char *>(flow) + entry(e) + at));
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -880,7 +883,9 @@ static int32_t predict_first(const pc_mixture &m, int32_t B)
 static void launch_predict(const pc_mixture &m, const PredictPlan &p, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace, hipStream_t s)
 {
     if (p.one) {
-        hipLaunchKernelGGL(k_predict_one, dim3((unsigned)((m.n_cats + 4 * one_rows(m) - 1) / (4 * one_rows(m)))), dim3(256), 0, s, m, tables, logp);
+        const dim3 grid((unsigned)((m.n_cats + 4 * one_rows(m) - 1) / (4 * one_rows(m))));
+        if ((int64_t)m.n_blocks * m.n_cats * m.K >= 64 << 20) hipLaunchKernelGGL(k_predict_one<true>, grid, dim3(256), 0, s, m, tables, logp);
+        else hipLaunchKernelGGL(k_predict_one<false>, grid, dim3(256), 0, s, m, tables, logp);
         return;
     }
     const int64_t rows = (m.n_cats + 31ll) / 32;

@@ -43,6 +43,12 @@ __device__ inline Pack<T> load_pack(const T *p)       // as one vector: element 
     return __builtin_bit_cast(Pack<T>, (pc_u32x4)*reinterpret_cast<const loose *>(p));
 }
 template <typename T>
+__device__ inline Pack<T> stream_pack(const T *p)     // what is not read again soon: the caches keep other things first
+{
+    typedef typename std::conditional<sizeof(T) == 2, pc_u32x4_at2, pc_u32x4_at4>::type loose;
+    return __builtin_bit_cast(Pack<T>, (pc_u32x4)__builtin_nontemporal_load(reinterpret_cast<const loose *>(p)));
+}
+template <typename T>
 __device__ inline void unpack_f32(const Pack<T> &r, float (&x)[Pack<T>::N])
 {
     const pc_u32x4 w = __builtin_bit_cast(pc_u32x4, r);
