@@ -136,7 +136,8 @@ __device__ inline float next_above(float t) { return key_value(order_key(t) + 1)
 // their elements are read again, one a lane, and those that reach it go to the wave's list: looking at every element of such a chunk
 // with a ballot each took 140 us where this takes 115 (256 x 16 x 50257 bf16).  A full list (rows in ascending order, ties) is cut to the n
 // best, whose last is the new bound; many lanes with such packs raise it by the chunk's own maxima.  Waves do not wait for each other between the first
-// bound and the end.  Bound by instructions in 16 bits (unpacking, maximum, exponential: 3.6 TB/s), by reading in 32 (the same rows 165 us, 5.0 TB/s).
+// bound and the end.  Bound by instructions in 16 bits (unpacking, maximum, exponential: 3.7 TB/s), by reading in 32 (the same rows 157 us, 5.2 TB/s;
+// not past the caches 165).
 // Five waves a SIMD: 115 us; four 120, six (spilling) 129.
 constexpr int kBeamPacks = 4, kWaveList = 256, kQueue = 64 * (kBeamPacks + 1), kBeamWaves = kBeamThreads / 64;
 template <typename T> constexpr int chunk_elements() { return kBeamThreads * kBeamPacks * Pack<T>::N; }
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(kBeamThreads, 5) void k_beam_rows(const BeamDev a, 
         auto fetch = [&](uint32_t base) {               // whole packs
 #pragma unroll
             for (int k = 0; k < kBeamPacks; ++k)
-                if (index(base, k) >= lo && index(base, k) + N <= hi) ahead[k] = *reinterpret_cast<const Pack<T> *>(__builtin_assume_aligned(grid + index(base, k), 16));
+                if (index(base, k) >= lo && index(base, k) + N <= hi) ahead[k] = stream_pack((const T *)__builtin_assume_aligned(grid + index(base, k), 16));
         };
         fetch(first);
         for (uint32_t base = first; base < hi; base += CHUNK) {
