@@ -106,8 +106,9 @@ __device__ inline floatx16 mfma(const uint4 &a, const uint4 &b, const floatx16 &
 // stages the weights [states][samples] into LDS as planes in operand order.  While a chunk is multiplied the next one is split and staged
 // and the one after it is on its way; one barrier a chunk.  Products of planes down to the last order kept (two planes: hi*hi + hi*lo + lo*hi;
 // three: all six down to 2^-24).  The samples are the instruction's rows, so that a store covers 32 neighbouring categories.  Bound by
-// reading the tables up to some 100 samples (4096 states x 50257: B = 16 173 us, 4.8 TB/s; B = 64 192), then by the matrix cores (B = 256 366 us:
-// 860 TFLOP/s of bf16 products; a large bf16 product reaches 1130).
+// reading the tables up to some 100 samples (4096 states x 50257: B = 16 173 us, 4.8 TB/s; B = 64 211), then by the matrix cores (B = 256 347 us:
+// 910 TFLOP/s of bf16 products; a large bf16 product reaches 1130).
+// Waves of 128 samples and more (READY) find the weights' planes ready: every workgroup splitting them anew took 385 us at B = 256.
 // A workgroup adds up `len` states from blockIdx.z * len on; several parts: the sums go to `sums` and k_predict_join takes the logarithm.
 // Where a group of four states begins in the tables and in the weights is looked up in LDS, a window of states at a time, so that
 // blocks need not be as long as a chunk; WHOLE: they are multiples of KC, one look-up serves a wave's part.
@@ -554,11 +555,11 @@ __global__ __launch_bounds__(64 * kPrepareWaves) void k_flow_prepare(const pc_mi
 // products (the terms of a flow have either sign and are few, so that nothing averages out; the fp32 matrix instructions took longer:
 // 4096 states x 50257, B = 256, gradients without zeros 1372 us).  While a step is multiplied the next one's operands are staged and the one
 // after is on its way.  Bound by the matrix cores' sustained rate from some 100 samples on (B = 256: 795 us, six products alone 557; making the
-// planes in every tile took 1010), before by reading the tables and writing their flows (B = 32: 371 us, 4.5 TB/s), which the products of a
+// planes in every tile took 1010), before by reading the tables and writing their flows (B = 32: 358 us, 4.7 TB/s), which the products of a
 // CU's other workgroups cover.
 // MARKED: operands as k_flow_prepare has left them.  Of a segment whose samples mostly have no gradient among the tile's categories (targets of
 // a few categories a sample: an EM step) only those that do are added up, their g / p made here and their weights taken by sample,
-// so that the columns of any sample are neighbours (64 categories a sample, B = 256: 438 us; gathered from the rows of m.weights 737,
+// so that the columns of any sample are neighbours (64 categories a sample, B = 256: 420 us; gathered from the rows of m.weights 737,
 // all samples 967).
 // LISTS: a table named by several blocks is the first one's: its column adds up all their weights, the others' columns do nothing, so every entry has
 // one writer.  The workgroups of a category tile follow one another on one XCD, whose cache keeps its g / p.
@@ -872,7 +873,7 @@ static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
 }
 
 // Samples of a first launch with the widest waves, the others in a second one: where half of such a wave would do for those (4096 states
-// x 50257, B = 257 490 us against 602).
+// x 50257, B = 257 502 us against 602).
 static int32_t predict_first(const pc_mixture &m, int32_t B)
 {
     if (B <= 256 || B % 256 == 0 || B % 256 > 128) return B;
