@@ -433,7 +433,7 @@ __device__ inline float flow_ratio(float logp, float g)
     constexpr float kLog2e = 1.44269504f, kRest = 1.92596299e-8f, kLn2 = 0.693147181f;    // log2(e) = kLog2e + kRest
     const float t = -logp * kLog2e, rest = fmaf(-logp, kRest, fmaf(-logp, kLog2e, -t));
     const float e = __builtin_amdgcn_exp2f(t);
-    return logp < kLogFltMin - 1e-3f ? 0.0f : (g * kDown) * fmaf(e, rest * kLn2, e);
+    return logp < kLogFltMin - 1e-3f ? 0.0f : g * (fmaf(e, rest * kLn2, e) * kDown);
 }
 
 // Column n of the flows: its first weight (-1: none, or another block's column does its table's work), its place in the flows for category 0,
