@@ -264,8 +264,7 @@ pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void
 
 /* Predictive distribution:  logp[b][c] = log sum_j sum_k weights[rows[j] + k][b] * tables[table[j]][c][k],  b < B, c < n_cats,
  * ld >= n_cats floats between the rows of logp.  A probability below FLT_MIN (a sample without weights: all of them) gives
- * -inf.  Sums are kept in fp32; products are off by at most 3 * 2^-16 of themselves where n_cats >= 4096 (whose
- * logarithms are large), else 2^-22. */
+ * -inf.  Sums are kept in fp32, products are off by at most 2^-22 of themselves, whatever batch a sample is in. */
 pc_status pc_predict_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace,
                      size_t workspace_bytes, void *stream);

@@ -65,9 +65,13 @@ __global__ __launch_bounds__(256) void k_predict_any(const pc_mixture m, const f
 __device__ inline int group_states(int K) { return (K + 3) & ~3; }      // of a block, with those repeated
 __device__ inline int group_start(int K, int k) { return min(k, K - 4); }
 
-// Operands are fp32; the matrix cores multiply bf16 and add in fp32.  An operand x is taken as a sum of bf16 planes, each the rounding of
-// what the planes before it leave: hi + lo keeps 2^-16 of x, hi + mid + lo 2^-24.  Weights (and tables) are scaled by 2^24 on the way, so that the
-// lower planes of numbers down to FLT_MIN are normal numbers; the scale is taken out of the fp32 sum, exactly.
+// Operands are fp32; the matrix cores multiply bf16 and add in fp32.  An operand x is taken as a sum of three bf16 planes, each the rounding of
+// what the planes before it leave: together they keep 2^-24 of x.  Of the products of planes the six down to 2^-16 are added up, those left out are
+// 2^-24 of the whole.  (Two planes and three products take half the time of the matrix cores and lose up to 3 * 2^-16 of a product.  Over many states that
+// averages out; where one state carries a sample, as the likely categories of a trained model have it, a logarithm near 0 would keep five digits.)
+// Weights (and tables) are scaled by 2^24 on the way, so that the lower planes of numbers down to FLT_MIN are normal numbers; the scale is taken
+// out of the fp32 sum, exactly.
+constexpr int kPlanes = 3;
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -77,20 +81,19 @@ constexpr float kUp = 16777216.0f, kDown = 1.0f / kUp;
 __device__ inline uint32_t round2(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2){a, b}, bf16x2)); }
 __device__ inline float low_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float high_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-// PLANES planes of eight numbers, 16 bytes each
-template <int PLANES>
-__device__ inline void split8(const float (&x)[8], uint4 (&plane)[PLANES])
+// the planes of eight numbers, 16 bytes each
+__device__ inline void split8(const float (&x)[8], uint4 (&plane)[kPlanes])
 {
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = x[i];
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p) {
+    for (int p = 0; p < kPlanes; ++p) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             w[i] = round2(v[2 * i], v[2 * i + 1]);
-            if (p + 1 < PLANES) { v[2 * i] -= low_of(w[i]); v[2 * i + 1] -= high_of(w[i]); }
+            if (p + 1 < kPlanes) { v[2 * i] -= low_of(w[i]); v[2 * i + 1] -= high_of(w[i]); }
         }
         plane[p] = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -104,22 +107,22 @@ __device__ inline floatx16 mfma(const uint4 &a, const uint4 &b, const floatx16 &
 // samples: waves with little to add up, bound by loads in flight) SPLIT waves of a workgroup share categories and add their sums at the end.
 // Each lane fetches its category's table row (8 contiguous states a step of 16, split in registers, read once from memory); the workgroup
 // stages the weights [states][samples] into LDS as planes in operand order.  While a chunk is multiplied the next one is split and staged
-// and the one after it is on its way; one barrier a chunk.  Products of planes down to the last order kept (two planes: hi*hi + hi*lo + lo*hi;
-// three: all six down to 2^-24).  The samples are the instruction's rows, so that a store covers 32 neighbouring categories.  Bound by
-// reading the tables up to some 100 samples (4096 states x 50257: B = 16 173 us, 4.8 TB/s; B = 64 211), then by the matrix cores (B = 256 347 us:
-// 910 TFLOP/s of bf16 products; a large bf16 product reaches 1130).
-// Waves of 128 samples and more (READY) find the weights' planes ready: every workgroup splitting them anew took 385 us at B = 256.
+// and the one after it is on its way; one barrier a chunk.
+// The samples are the instruction's rows, so that a store covers 32 neighbouring categories.  Bound by reading the tables and splitting them up to some
+// 64 samples (4096 states x 50257: B = 16 221 us, 3.7 TB/s; B = 64 249), then by the matrix cores (B = 128 341 us; B = 256 590: 1070 TFLOP/s of
+// bf16 products, six to a product; a large bf16 product reaches 1130).
+// Waves of 128 samples and more (READY) find the weights' planes ready: every workgroup splitting them anew took 382 us at B = 128, 624 at B = 256.
 // A workgroup adds up `len` states from blockIdx.z * len on; several parts: the sums go to `sums` and k_predict_join takes the logarithm.
 // Where a group of four states begins in the tables and in the weights is looked up in LDS, a window of states at a time, so that
 // blocks need not be as long as a chunk; WHOLE: they are multiples of KC, one look-up serves a wave's part.
 constexpr int kWindow = 2048;
-template <int NT, int WAVES, int SPLIT, int KC, int PLANES, bool WHOLE>
-__global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 3 : 4) void k_predict(const pc_mixture m, const float *__restrict__ tables, int32_t B,
+template <int NT, int WAVES, int SPLIT, int KC, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_predict(const pc_mixture m, const float *__restrict__ tables, int32_t B,
                                                                         float *__restrict__ logp, int64_t ld, int32_t len, float *__restrict__ sums, const pc_u32x4 *__restrict__ ready)
 {
     constexpr bool READY = NT >= 4;
     constexpr int TH = 64 * WAVES, NB = 32 * NT, STEPS = KC / 16, KW = KC * SPLIT, TASKS = NB * KW / 8, FT = (TASKS + TH - 1) / TH;
-    __shared__ uint4 planes[2][PLANES][KW / 8][NB];   // [buffer][plane][8 states][sample]
+    __shared__ uint4 planes[2][kPlanes][KW / 8][NB];   // [buffer][plane][8 states][sample]
     __shared__ int64_t t_at[kWindow / 4], w_at[kWindow / 4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5, part = wave % SPLIT;
     const int Kg = group_states(m.K), first = blockIdx.z * len, H = min(m.n_blocks * Kg - first, len), c0 = (blockIdx.x * (WAVES / SPLIT) + wave / SPLIT) * 32, b0 = blockIdx.y * NB;
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     // split.  A chunk behind the last state is fetched and staged like any other, and not used.
     Pack<float> t_raw[STEPS][2];
     float w_raw[READY ? 1 : FT][8];
-    pc_u32x4 w_ready[READY ? FT : 1][PLANES];
+    pc_u32x4 w_ready[READY ? FT : 1][kPlanes];
     const int columns = gridDim.y * NB, groups = (m.n_blocks * Kg + 7) / 8;
     uint32_t t_mask[WHOLE ? 1 : STEPS][2];
     int w_skip[FT][2];                                 // 4: all
@@ -163,7 +166,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
         if (READY) {
             const int g = min((first + n0) / 8 + task_g[f], groups - 1);
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) w_ready[f][p] = (ready + ((int64_t)p * groups + g) * columns)[b0 + task_b[f]];
+            for (int p = 0; p < kPlanes; ++p) w_ready[f][p] = (ready + ((int64_t)p * groups + g) * columns)[b0 + task_b[f]];
             return;
         }          // of the chunk that begins with state `first` + n0
         const int g0 = n0 % kWindow / 4;
@@ -204,20 +207,20 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     auto stage_weights = [&](int buf, int f) {
         if (READY) {
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) planes[buf][p][task_g[f]][task_b[f]] = __builtin_bit_cast(uint4, w_ready[f][p]);
+            for (int p = 0; p < kPlanes; ++p) planes[buf][p][task_g[f]][task_b[f]] = __builtin_bit_cast(uint4, w_ready[f][p]);
             return;
         }
         if (!wave_stages[f]) return;
         float x[8];
-        uint4 pl[PLANES];
+        uint4 pl[kPlanes];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = i % 4 >= w_skip[f][i / 4] ? w_raw[f][i] * kUp : 0.0f;
         split8(x, pl);
         if (NT > 1 || task_g[f] >= 0)
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) planes[buf][p][task_g[f]][task_b[f]] = pl[p];
+            for (int p = 0; p < kPlanes; ++p) planes[buf][p][task_g[f]][task_b[f]] = pl[p];
     };
-    uint4 tp[STEPS][PLANES];
+    uint4 tp[STEPS][kPlanes];
     auto split_tables = [&](int s) {
         float x[8];
 #pragma unroll
@@ -244,17 +247,17 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
     for (int n0 = 0, buf = 0; n0 < H; n0 += KW, buf ^= 1) {
         const int next = n0 + 2 * KW;
         if (next % kWindow == 0) { fill_window(next); __syncthreads(); }                   // the barrier before: all have read the last one
-        uint4 cp[STEPS][PLANES], wp[2][G][PLANES];
+        uint4 cp[STEPS][kPlanes], wp[2][G][kPlanes];
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) cp[s][p] = tp[s][p];
+            for (int p = 0; p < kPlanes; ++p) cp[s][p] = tp[s][p];
         auto operands = [&](int slice) {
             const int s = slice / (NT / G), t = slice % (NT / G) * G;
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) wp[slice & 1][g][p] = planes[buf][p][part * (KC / 8) + 2 * s + half][32 * (t + g) + col];
+                for (int p = 0; p < kPlanes; ++p) wp[slice & 1][g][p] = planes[buf][p][part * (KC / 8) + 2 * s + half][32 * (t + g) + col];
         };
         auto tables_on = [&]() {
 #pragma unroll
@@ -272,7 +275,7 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
             const int s = slice / (NT / G), t = slice % (NT / G) * G, o = slice & 1;
             if (slice + 1 < SLICES) operands(slice + 1);
 #pragma unroll
-            for (int sum = PLANES - 1; sum >= 0; --sum)  // the small products first
+            for (int sum = kPlanes - 1; sum >= 0; --sum)  // the small products first
 #pragma unroll
                 for (int p = sum; p >= 0; --p)
 #pragma unroll
@@ -320,7 +323,6 @@ __global__ __launch_bounds__(64 * WAVES, NT == 8 || PLANES == 3 ? 2 : NT == 4 ? 
 }
 
 // The weights as planes in operand order, ready[plane][8 states][sample]: what k_predict with wide waves stages as it is.
-template <int PLANES>
 __global__ __launch_bounds__(256) void k_predict_ready(const pc_mixture m, int32_t B, int32_t columns, uint4 *__restrict__ ready)
 {
     const int Kg = group_states(m.K), groups = (m.n_blocks * Kg + 7) / 8, b = blockIdx.y * 64 + threadIdx.x % 64, g = blockIdx.x * 4 + threadIdx.x / 64;
@@ -338,10 +340,10 @@ __global__ __launch_bounds__(256) void k_predict_ready(const pc_mixture m, int32
             x[4 * q + i] = i >= skip ? v * kUp : 0.0f;
         }
     }
-    uint4 pl[PLANES];
+    uint4 pl[kPlanes];
     split8(x, pl);
 #pragma unroll
-    for (int p = 0; p < PLANES; ++p) ready[((int64_t)p * groups + g) * columns + b] = pl[p];
+    for (int p = 0; p < kPlanes; ++p) ready[((int64_t)p * groups + g) * columns + b] = pl[p];
 }
 
 // Log-probabilities from the sums over `parts` parts of the states.
@@ -840,16 +842,15 @@ __global__ __launch_bounds__(256) void k_flow_join(const pc_mixture m, const flo
 static int64_t one_rows(const pc_mixture &m) { return 64 / ((m.K + 3) / 4) * kOneRows; }      // categories of a wave of k_predict_one
 
 // How a prediction is launched.
-// One sample of many categories: no matrix cores (100 states x 20 blocks x 50257 80 us against 101, 32 states x 8 14 against 18; 4096 states 156 and
-// 154, 8192 states x 20000 133 and 119; two samples of 4096 163 and 156), where that makes waves enough for two to a CU.
-// Two planes an operand where log-probabilities are large (many categories), three where they are not: an error of 2^-18 of a probability
-// is 10^-6 of a logarithm of -4, but as much as the logarithm's own rounding allows at -10.
-// Samples a wave: as many of 256 as there are, so that the tables are read once; fewer where that leaves a SIMD without a wave (the
-// tables of few categories stay in the caches).
+// One sample of many categories: no matrix cores (100 states x 20 blocks x 50257 78 us against 123, 32 states x 8 18 against 31; 4096 states 146 and
+// 246, 8192 states x 20000 127 and 229), where that makes waves enough for two to a CU.
+// Samples a wave: as many of 256 as there are, so that the tables are read once; 128 below 4096 categories (256 and 128: 4096 states x 4000, B = 256
+// 78 us and 74, x 9000 128 and 139, x 50257 590 and 690); 64 from 17 samples on (64 and 32: 4096 states x 50257, B = 24 235 us and 275, B = 16 237 and
+// 221); fewer where that leaves a SIMD without a wave (the tables of few categories stay in the caches).
 // Where there is less than a workgroup to a CU and the states are many (1024: an exchange and a second launch take some 4 us) they are dealt out
-// in parts of at least 256, as many as fill the GPU once, whose sums k_predict_join adds up (4096 states x 256, B = 256 22 us against 61;
-// x 5000 63 against 144; x 16000, 2048 states, B = 500 124 against 135; with more workgroups, 1024 states x 50257, B = 64 66 against 49).
-struct PredictPlan { bool one, exact; int32_t nt, len, parts, columns; size_t sums, bytes; };
+// in parts of at least 256, as many as fill the GPU once, whose sums k_predict_join adds up (4096 states x 256, B = 256 24 us against 64;
+// x 5000 89 against 468; x 16000, 2048 states, B = 500 203 against 262; with more workgroups, 1024 states x 50257, B = 64 84 against 69).
+struct PredictPlan { bool one; int32_t nt, len, parts, columns; size_t sums, bytes; };
 static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
 {
     PredictPlan p{};
@@ -857,23 +858,22 @@ static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
     p.one = B == 1 && m.n_cats >= 512 * one_rows(m);
     if (p.one) return p;
     const int64_t rows = (m.n_cats + 31ll) / 32, H = (int64_t)m.n_blocks * ((m.K + 3) / 4 * 4), most = H < 1024 ? 1 : H / 256;
-    p.exact = m.n_cats < 4096;
-    p.nt = B > 128 && !p.exact ? 8 : B > 64 ? 4 : B > 32 ? 2 : 1;
+    p.nt = B > 128 && m.n_cats >= 4096 ? 8 : B > 64 ? 4 : B > 16 ? 2 : 1;
     const auto columns = [&] { return (B + 32ll * p.nt - 1) / (32 * p.nt); };
     while (p.nt > 1 && rows * columns() * most < 1024) p.nt /= 2;
     const int64_t groups = (p.nt == 8 ? (rows + 7) / 8 : p.nt > 1 ? (rows + 3) / 4 : rows) * columns();
-    const int64_t slots = 256 * (p.nt == 8 ? 1 : p.nt == 4 ? (p.exact ? 2 : 3) : p.nt == 2 ? (p.exact ? 3 : 4) : (p.exact ? 2 : 4));
+    const int64_t slots = 256 * (p.nt == 8 ? 1 : p.nt == 2 ? 3 : 2);
     const int64_t want = groups < 256 ? std::min(slots / groups, most) : 1;
     p.len = (int32_t)((H + want * 128 - 1) / (want * 128) * 128);
     p.parts = (int32_t)((H + p.len - 1) / p.len);
     p.columns = (int32_t)(columns() * 32 * p.nt);
-    p.sums = p.nt >= 4 ? (size_t)(p.exact ? 3 : 2) * ((H + 7) / 8) * p.columns * 16 : 0;
+    p.sums = p.nt >= 4 ? (size_t)kPlanes * ((H + 7) / 8) * p.columns * 16 : 0;
     p.bytes = p.sums + (p.parts > 1 ? (size_t)p.parts * B * m.n_cats * 4 : 0);
     return p;
 }
 
 // Samples of a first launch with the widest waves, the others in a second one: where half of such a wave would do for those (4096 states
-// x 50257, B = 257 502 us against 602).
+// x 50257, B = 257 712 us against 1037, B = 384 947 against 1089).
 static int32_t predict_first(const pc_mixture &m, int32_t B)
 {
     if (B <= 256 || B % 256 == 0 || B % 256 > 128) return B;
@@ -895,22 +895,18 @@ static void launch_predict(const pc_mixture &m, const PredictPlan &p, const floa
     if (p.nt >= 4) {
         const int64_t groups = ((int64_t)m.n_blocks * ((m.K + 3) / 4 * 4) + 7) / 8;
         const dim3 grid((unsigned)((groups + 3) / 4), (unsigned)((p.columns + 63) / 64));
-        if (p.exact) hipLaunchKernelGGL(k_predict_ready<3>, grid, dim3(256), 0, s, m, B, p.columns, ready);
-        else hipLaunchKernelGGL(k_predict_ready<2>, grid, dim3(256), 0, s, m, B, p.columns, ready);
+        hipLaunchKernelGGL(k_predict_ready, grid, dim3(256), 0, s, m, B, p.columns, ready);
     }
-#define PC_PREDICT(NT, WAVES, SPLIT, KC, PLANES)                                                                               \
-    if (p.nt == NT && p.exact == (PLANES == 3)) {                                                                              \
+#define PC_PREDICT(NT, WAVES, SPLIT, KC)                                                                                       \
+    if (p.nt == NT) {                                                                                                          \
         const dim3 grid((unsigned)((rows + WAVES / SPLIT - 1) / (WAVES / SPLIT)), (unsigned)((B + 32 * NT - 1) / (32 * NT)), p.parts);  \
-        if (m.K % KC == 0) hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, true>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums, (const pc_u32x4 *)ready); \
-        else hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, PLANES, false>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums, (const pc_u32x4 *)ready); \
+        if (m.K % KC == 0) hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, true>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums, (const pc_u32x4 *)ready); \
+        else hipLaunchKernelGGL((k_predict<NT, WAVES, SPLIT, KC, false>), grid, dim3(64 * WAVES), 0, s, m, tables, B, logp, ld, p.len, sums, (const pc_u32x4 *)ready); \
     }
-    PC_PREDICT(8, 8, 1, 32, 2)
-    PC_PREDICT(4, 4, 1, 32, 2)
-    PC_PREDICT(2, 4, 1, 32, 2)
-    PC_PREDICT(1, 4, 4, 32, 2)
-    PC_PREDICT(4, 4, 1, 32, 3)
-    PC_PREDICT(2, 4, 1, 32, 3)
-    PC_PREDICT(1, 4, 4, 32, 3)
+    PC_PREDICT(8, 8, 1, 32)
+    PC_PREDICT(4, 4, 1, 32)
+    PC_PREDICT(2, 4, 1, 32)
+    PC_PREDICT(1, 4, 4, 32)
 #undef PC_PREDICT
     if (sums) {
         const int64_t n = (int64_t)B * m.n_cats;
