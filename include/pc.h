@@ -314,7 +314,8 @@ pc_status pc_distill_backward(const pc_distill *d, const float *stats, const flo
                               int64_t dstudent_ld, void *stream);
 
 /* Beam search: of all beams and categories of a group the n_out best.  Candidate (beam, c) has the score
- * running[beam] + z, z = scores[beam][c], minus log sum_c' exp(scores[beam][c']) where `normalise` (rows of logits), taken in 64 bits.
+ * running[beam] + z, z = scores[beam][c], minus log sum_c' exp(scores[beam][c']) where `normalise` (rows of logits), added in 64 bits.  The exponentials
+ * are fp32, their sum over a row and its logarithm 64 bits: it is off by at most 2^-17 (1e-7 for 50257 normal logits), and beams whose scores lie closer may change places.
  * A finished beam (done != 0) has the one candidate done_token with z = 0; its row is not read.  Order: higher score, then lower
  * beam, then (within a beam) higher z, then lower category.  Candidates that are no numbers or whose beam's running score is
  * no number below +inf count as -inf, as do all of a row whose log-normaliser is no finite number; candidates of -inf come last, by

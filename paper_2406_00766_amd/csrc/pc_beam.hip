@@ -141,7 +141,11 @@ __device__ inline float next_above(float t) { return key_value(order_key(t) + 1)
 // Five waves a SIMD: 115 us; four 120, six (spilling) 129.
 constexpr int kBeamPacks = 4, kWaveList = 256, kQueue = 64 * (kBeamPacks + 1), kBeamWaves = kBeamThreads / 64;
 template <typename T> constexpr int chunk_elements() { return kBeamThreads * kBeamPacks * Pack<T>::N; }
-struct RowPart { float m; float pad; double sum; };    // maximum and sum of exp(z - m) of a segment
+struct RowPart { float m; float pad; double sum; };    // reference and sum of exp(z - m) of a segment
+// The log-normaliser: exponentials in fp32, added in fp32 within a lane's part of a chunk (16 or 32 of them) and in 64 bits from there on.  A wave's
+// reference follows its maximum only where that is more than this above it: a factor in fp32 for each new maximum would be an error for each chunk of a
+// row that rises slowly, this way an entry meets one for each 8 that the maximum comes to lie above it.
+constexpr float kBeamSlack = 8.0f;
 
 // A wave's list and its length.
 struct WaveList {
@@ -192,7 +196,8 @@ __global__ __launch_bounds__(kBeamThreads, 5) void k_beam_rows(const BeamDev a, 
         const int off = elements_off(z);
         const T *grid = z - off;
         const uint32_t first = (uint32_t)(task % n_seg) * (uint32_t)seg_len, hi = min((uint32_t)off + (uint32_t)a.n_cats, first + (uint32_t)seg_len), lo = max((uint32_t)off, first);
-        float m = PC_NEG_INF_F, sum = 0.0f, t = PC_NEG_INF_F;
+        float m = PC_NEG_INF_F, t = PC_NEG_INF_F;      // m: reference of the wave's exponentials
+        double sum = 0.0;
         bool fresh = false;                            // t is reached by n categories of this chunk or before, not above all of them
         WaveList mine{lists[wave], 0};
         int queued = 0;                                // packs of the wave's queue
@@ -238,7 +243,11 @@ __global__ __launch_bounds__(kBeamThreads, 5) void k_beam_rows(const BeamDev a, 
             }
             if (base + CHUNK < hi) fetch(base + CHUNK);
             if (a.normalise) {
-                if (top > m) { sum *= exp2f((m - top) * PC_LOG2E_F); m = top; }
+                if (__any(top > m + kBeamSlack)) {
+                    const float higher = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(wave_all(top, [](float x, float y) { return fmaxf(x, y); }))));
+                    sum *= __builtin_amdgcn_exp2f((m - higher) * PC_LOG2E_F);
+                    m = higher;
+                }
                 const float at = m == PC_NEG_INF_F ? 0.0f : m;
                 float part = 0.0f;
 #pragma unroll
@@ -286,9 +295,7 @@ __global__ __launch_bounds__(kBeamThreads, 5) void k_beam_rows(const BeamDev a, 
         }
         uint64_t v = mine.cut(n);
         if (wave > 0) lists[wave][lane] = v;
-        float all = m;
-        for (int d = 32; d > 0; d >>= 1) all = fmaxf(all, __shfl_xor(all, d));
-        if (lane == 0) wave_m[wave] = all;
+        if (lane == 0) wave_m[wave] = m;
         __syncthreads();
         if (wave == 0) {
 #pragma unroll
@@ -296,8 +303,9 @@ __global__ __launch_bounds__(kBeamThreads, 5) void k_beam_rows(const BeamDev a, 
             if (lane < n) best[task * n + lane] = v;
         }
         if (a.normalise) {
+            float all = m;
             for (int w = 0; w < kBeamWaves; ++w) all = fmaxf(all, wave_m[w]);
-            double total = (double)sum * (m == PC_NEG_INF_F ? 1.0 : (double)exp2f((m - all) * PC_LOG2E_F));
+            double total = sum * (m == PC_NEG_INF_F ? 1.0 : (double)exp2f((m - all) * PC_LOG2E_F));
             for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
             if (lane == 0) wave_sum[wave] = total;
             __syncthreads();
