@@ -291,7 +291,7 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
  * ids outside [0, n_cats) are no entries (padding of short lists: -1), as are teacher logits of -inf; a category listed twice counts
  * twice.  A row without entries has loss 0 and gradient 0 whatever the student's row holds.  A student logit of -inf has p = 0;
  * loss is +inf where such a category, or any in a row of nothing else, is listed with q > 0.  NaN and +inf in a row make its
- * results NaN (a `normalised` row: only where they are listed). */
+ * results NaN (a `normalised` row: its loss, where they are listed; its gradient is -q whatever it holds). */
 #define PC_MAX_TOP 1024
 typedef struct {
     int64_t rows;

@@ -185,7 +185,7 @@ __global__ __launch_bounds__((Group<WAVES, LONG>::BLOCK)) void k_distill_rows(co
         for (int i = 0; i < G::LIST; ++i)
             if (list.id[i] >= 0 && !(list.q[i] == 0.0f)) {
                 const float v = listed[i];
-                const float logp = d.normalised ? v : m == PC_NEG_INF_F ? m : (v - m) * d.inv_T - log_s;
+                const float logp = d.normalised ? (v == __builtin_inff() ? __builtin_nanf("") : v) : m == PC_NEG_INF_F ? m : (v - m) * d.inv_T - log_s;
                 part += list.q[i] * (list.logq[i] - logp);
             }
         part = G::list_all(part, lds, add2);
