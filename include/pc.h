@@ -300,7 +300,7 @@ typedef struct {
     const int32_t *ids;                          int64_t ids_ld;
     const void *teacher;  int32_t teacher_type;  int64_t teacher_ld;
     const float *teacher_lse;                    /* [rows] or NULL                                                  */
-    float temperature;                           /* > 0                                                             */
+    float temperature;                           /* finite, and log2(e) / temperature too: at least 4.3e-39         */
     int32_t normalised;
 } pc_distill;
 pc_status pc_distill_workspace_bytes(const pc_distill *d, size_t *bytes);

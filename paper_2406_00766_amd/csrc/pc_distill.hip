@@ -328,8 +328,8 @@ static pc_status check_distill(const pc_distill *d)
     if (d->n_cats < 1) return fail(PC_ERR_ARG, "n_cats must be positive");
     if (d->top < 1 || d->top > PC_MAX_TOP) return fail(PC_ERR_ARG, "top must be in 1 .. PC_MAX_TOP");
     if (!type_known(d->student_type) || !type_known(d->teacher_type)) return fail(PC_ERR_ARG, "unknown element type");
-    if (!(d->temperature > 0.0f) || std::isinf(d->temperature) || std::isinf(1.0f / d->temperature))
-        return fail(PC_ERR_ARG, "temperature and its reciprocal must be positive and finite");
+    if (!(d->temperature > 0.0f) || std::isinf(d->temperature) || std::isinf(1.0f / d->temperature * PC_LOG2E_F))   // a factor of exponents
+        return fail(PC_ERR_ARG, "temperature and log2(e) / temperature must be positive and finite");
     if (d->normalised && d->temperature != 1.0f) return fail(PC_ERR_ARG, "normalised rows have temperature 1");
     if (d->student_ld < d->n_cats) return fail(PC_ERR_ARG, "student_ld is smaller than n_cats");
     if (d->ids_ld < d->top || d->teacher_ld < d->top) return fail(PC_ERR_ARG, "ids_ld or teacher_ld is smaller than top");
