@@ -263,7 +263,7 @@ pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void
                          pc_mixture *out);
 
 /* Predictive distribution:  logp[b][c] = log sum_j sum_k weights[rows[j] + k][b] * tables[table[j]][c][k],  b < B, c < n_cats,
- * ld >= n_cats floats between the rows of logp.  A probability below FLT_MIN (a sample without weights: all of them) gives
+ * ld >= n_cats floats between the rows of logp, which overlaps neither tables nor weights.  A probability below FLT_MIN (a sample without weights: all of them) gives
  * -inf.  Sums are kept in fp32, products are off by at most 2^-22 of themselves, whatever batch a sample is in. */
 pc_status pc_predict_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace,
@@ -275,8 +275,8 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
  * which is the objective's gradient with respect to log tables[t][c][k];  table_flow = scale * flow for the tables that the mixture
  * names, added to what is there where `accumulate` is set.  With dlogp = -q (a loss -sum q logp, q >= 0) and scale = -1 these are
  * the flows of an EM step on soft targets, ready for pc_em_step.  Entries of logp below log FLT_MIN add nothing.  Sums are kept in
- * fp32, products weights * dlogp / exp(logp) are off by at most 2^-22 of themselves (by 2^-102 of the weight where that is more).  table_flow is 16-byte aligned, laid out like the tables, and not the tables themselves; flows of tables that
- * no block names stay as they are. */
+ * fp32, products weights * dlogp / exp(logp) are off by at most 2^-22 of themselves (by 2^-102 of the weight where that is more).  table_flow is 16-byte aligned, laid out like the tables, and
+ * overlaps neither them nor the weights, logp or dlogp (PC_ERR_ARG); flows of tables that no block names stay as they are. */
 pc_status pc_predict_backward_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t B, const float *logp, int64_t logp_ld,
                               const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow,

@@ -374,12 +374,6 @@ static void with_group(const pc_distill *d, Rule, F f)
 template <typename G>
 static dim3 row_grid(int64_t rows) { return dim3((unsigned)std::min<int64_t>((rows + G::ROWS - 1) / G::ROWS, 1 << 20)); }
 
-// first and last byte of `rows` rows
-static bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
-{
-    return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
-}
-
 }  // namespace pc
 
 using namespace pc;
@@ -427,8 +421,8 @@ pc_status pc_distill_backward(const pc_distill *d, const float *stats, const flo
     if (dstudent_ld < d->n_cats) return fail(PC_ERR_ARG, "dstudent_ld is smaller than n_cats");
     const int64_t e = type_bytes(d->student_type);
     if (!aligned_to(stats, 4) || !aligned_to(dloss, 4) || !aligned_to(dstudent, e)) return fail(PC_ERR_ARG, "arrays must be aligned to their elements");
-    const int64_t in = ((d->rows - 1) * d->student_ld + d->n_cats) * e, out = ((d->rows - 1) * dstudent_ld + d->n_cats) * e;
-    if (overlap(d->student, in, dstudent, out) && !(d->student == dstudent && d->student_ld == dstudent_ld))
+    if (overlap(d->student, span_bytes(d->rows, d->student_ld, d->n_cats, e), dstudent, span_bytes(d->rows, dstudent_ld, d->n_cats, e)) &&
+        !(d->student == dstudent && d->student_ld == dstudent_ld))
         return fail(PC_ERR_ARG, "dstudent overlaps the student's rows without being them");
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {

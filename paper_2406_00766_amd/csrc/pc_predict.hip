@@ -965,6 +965,11 @@ static pc_status check_mixture(const pc_mixture *m, int32_t B)
         return fail(PC_ERR_ARG, "weights, rows and table must be 4-byte aligned");
     return PC_OK;
 }
+// What a call writes may not be what it reads: workgroups read the weights and tables as long as others write.
+static bool over_operands(const pc_mixture &m, const float *tables, int32_t B, const float *out, int64_t bytes)
+{
+    return overlap(out, bytes, tables, (int64_t)m.n_tables * m.n_cats * m.K * 4) || overlap(out, bytes, m.weights, span_bytes(m.n_rows, m.stride, B, 4));
+}
 
 }  // namespace pc
 
@@ -990,15 +995,16 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
     if (!aligned_to(tables, 16)) return fail(PC_ERR_ARG, "tables must be 16-byte aligned");
     if (ld < m->n_cats) return fail(PC_ERR_ARG, "ld is smaller than n_cats");
     if (!aligned_to(logp, 4)) return fail(PC_ERR_ARG, "logp must be 4-byte aligned");
+    size_t need = 0;
+    pc_predict_workspace_bytes(m, B, &need);
+    if (workspace_bytes < need) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_workspace_bytes");
+    if (need && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
+    if (over_operands(*m, tables, B, logp, span_bytes(B, ld, m->n_cats, 4))) return fail(PC_ERR_ARG, "logp overlaps the tables or the weights");
     if (m->K < 4) {
         const dim3 grid((unsigned)((m->n_cats + 63ll) / 64), (unsigned)((B + 63) / 64));
         hipLaunchKernelGGL(k_predict_any, grid, dim3(256), 0, (hipStream_t)stream, *m, tables, B, logp, ld);
         return launched();
     }
-    size_t need = 0;
-    pc_predict_workspace_bytes(m, B, &need);
-    if (workspace_bytes < need) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_workspace_bytes");
-    if (need && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
     const int32_t first = predict_first(*m, B);
     launch_predict(*m, predict_plan(*m, first), tables, first, logp, ld, workspace, (hipStream_t)stream);
     if (first < B) {
@@ -1035,6 +1041,10 @@ pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t 
     const FlowSpace f = flow_space(*m, B);
     if (workspace_bytes < f.bytes) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_predict_backward_workspace_bytes");
     if (f.bytes && (!workspace || !aligned_to(workspace, 16))) return fail(PC_ERR_ARG, "workspace must be 16-byte aligned");
+    const int64_t flow_bytes = (int64_t)m->n_tables * m->n_cats * m->K * 4;
+    if (over_operands(*m, tables, B, table_flow, flow_bytes) || overlap(table_flow, flow_bytes, logp, span_bytes(B, logp_ld, m->n_cats, 4)) ||
+        overlap(table_flow, flow_bytes, dlogp, span_bytes(B, dlogp_ld, m->n_cats, 4)))
+        return fail(PC_ERR_ARG, "table_flow overlaps the tables, the weights, logp or dlogp");
     char *base = (char *)workspace;
     const FlowPrep prep{(float *)base, (uint32_t *)(base + f.marks), (pc_u32x4 *)(base + f.wp), (pc_u32x4 *)(base + f.rp), f.parts > 1 ? (float *)(base + f.sums) : nullptr, f.part};
     const bool wide = flow_wide(*m);

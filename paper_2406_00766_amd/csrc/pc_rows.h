@@ -116,6 +116,13 @@ inline int64_t type_bytes(int32_t type) { return type == PC_F32 ? 4 : 2; }
 inline bool type_known(int32_t type) { return type == PC_F32 || type == PC_BF16 || type == PC_F16; }
 inline bool aligned_to(const void *p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
+// from the first byte of `rows` rows of n elements, ld apart, to their last
+inline int64_t span_bytes(int64_t rows, int64_t ld, int64_t n, int64_t element) { return ((rows - 1) * ld + n) * element; }
+inline bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
+{
+    return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
+}
+
 // f(element) for the C++ type of `type`
 template <typename F>
 inline void with_type(int32_t type, F f)

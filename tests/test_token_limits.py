@@ -8,6 +8,8 @@ import pytest
 from paper_2406_00766_amd import binding as pcb
 from tests.test_token_refusals import P, distill, status
 
+FAR = 1 << 24                                              # arrays this far apart do not touch each other
+
 
 @pytest.mark.parametrize("temperature,want", [(4.3e-39, "PC_OK"), (4.2e-39, "PC_ERR_ARG"), (3e-39, "PC_ERR_ARG"), (1e38, "PC_OK")])
 def test_temperatures_whose_exponents_overflow_are_refused(temperature, want):
@@ -19,3 +21,23 @@ def test_temperatures_whose_exponents_overflow_are_refused(temperature, want):
     if want != "PC_OK":
         assert status(pcb.lib().pc_distill_forward(C.byref(d), None, 0, P, P, None)) == want
         assert status(pcb.lib().pc_distill_backward(C.byref(d), P, None, 1.0, P << 4, 50, None)) == want
+
+
+def flows(table_flow, tables=FAR, weights=2 * FAR, logp=3 * FAR, dlogp=4 * FAR, ld=10):
+    m = pcb.pc_mixture(K=32, n_blocks=4, n_cats=10, n_tables=4, n_rows=128, stride=64, weights=weights, rows=None, table=None)
+    return status(pcb.lib().pc_predict_backward(C.byref(m), tables, 16, logp, ld, dlogp, 10, 1.0, 1, table_flow, None, 0, None))
+
+
+def test_flows_that_overlap_what_they_are_made_of_are_refused():
+    size = 4 * 10 * 32 * 4                                 # of tables and flows; 128 rows of weights; 16 rows of 10 categories
+    for table_flow in (FAR, FAR + size - 16, FAR - size + 16, 2 * FAR, 2 * FAR + (127 * 64 + 16) * 4 - 16, 3 * FAR + 15 * 40 + 32, 4 * FAR - 16):
+        assert flows(table_flow) == "PC_ERR_ARG", table_flow
+    assert flows(3 * FAR + 15 * 400 + 32, ld=100) == "PC_ERR_ARG"      # the last of logp's strided rows
+    assert "overlap" in (pcb.lib().pc_last_error() or b"").decode()
+
+
+def test_log_probabilities_that_overlap_what_they_are_made_of_are_refused():
+    m = pcb.pc_mixture(K=32, n_blocks=4, n_cats=10, n_tables=4, n_rows=128, stride=64, weights=2 * FAR, rows=None, table=None)
+    for logp in (FAR, FAR + 4 * 10 * 32 * 4 - 4, FAR - 16 * 40 + 4, 2 * FAR, 2 * FAR + (127 * 64 + 16) * 4 - 4):
+        assert status(pcb.lib().pc_predict(C.byref(m), FAR, 16, logp, 10, None, 0, None)) == "PC_ERR_ARG", logp
+        assert "overlap" in (pcb.lib().pc_last_error() or b"").decode()
