@@ -331,7 +331,8 @@ typedef struct {
     int32_t done_token;
 } pc_beam;
 pc_status pc_beam_workspace_bytes(const pc_beam *a, size_t *bytes);
-/* out_scores (fp32), parents (beam within the group), tokens: device, [groups][n_out], best first.  workspace: 16-byte aligned. */
+/* out_scores (fp32), parents (beam within the group), tokens: device, [groups][n_out], best first.  workspace: 16-byte aligned.  Outputs overlap neither
+ * each other nor scores, running or done (PC_ERR_ARG), but out_scores may be `running` where n_out == beams. */
 pc_status pc_beam_select(const pc_beam *a, void *workspace, size_t workspace_bytes, float *out_scores, int32_t *parents,
                          int32_t *tokens, void *stream);
 /* What each survivor takes along: row g * n_out + i of dst = row g * beams + parents[g][i] of src, for up to PC_MAX_STATES arrays

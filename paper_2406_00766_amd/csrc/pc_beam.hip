@@ -324,7 +324,7 @@ __global__ __launch_bounds__(kBeamThreads, 5) void k_beam_rows(const BeamDev a, 
 // second of any.  Bound by its chain of loads and comparisons (it moves a few KB): sorting the entries 64 at a time took 10 to 16 us.
 constexpr int kJoinWaves = 16, kRanked = 256;
 __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(const BeamDev a, int32_t n_seg, const uint64_t *__restrict__ best,
-                                                               const RowPart *__restrict__ parts, float *__restrict__ out_scores,
+                                                               const RowPart *__restrict__ parts, float *out_scores,
                                                                int32_t *__restrict__ parents, int32_t *__restrict__ tokens)
 {
     __shared__ Cand lists[kJoinWaves][64];             // or the candidates that are ranked
@@ -556,6 +556,15 @@ pc_status pc_beam_select(const pc_beam *a, void *workspace, size_t workspace_byt
     size_t need = 0;
     pc_beam_workspace_bytes(a, &need);
     if (workspace_bytes < need) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_beam_workspace_bytes");
+    // groups write while others read; a group reads its own running scores before it writes
+    const int64_t rows = (int64_t)a->groups * a->beams, out_bytes = (int64_t)a->groups * a->n_out * 4;
+    const void *const outs[] = {out_scores, parents, tokens};
+    for (int i = 0; i < 3; ++i) {
+        const bool in_place = i == 0 && out_scores == a->running && a->n_out == a->beams;
+        if (overlap(outs[i], out_bytes, a->scores, span_bytes(rows, a->scores_ld, a->n_cats, type_bytes(a->scores_type))) || (a->done && overlap(outs[i], out_bytes, a->done, rows)) ||
+            (a->running && !in_place && overlap(outs[i], out_bytes, a->running, rows * 4)) || overlap(outs[i], out_bytes, outs[(i + 1) % 3], out_bytes))
+            return fail(PC_ERR_ARG, "outputs overlap scores, running, done or each other");
+    }
     const BeamDev dev{a->groups, a->beams, a->n_cats, a->n_out, a->scores, a->scores_ld, a->normalise != 0, a->running, a->done, a->done_token};
     const Segments seg = segments_of(a);
     uint64_t *best = (uint64_t *)workspace;

@@ -66,3 +66,18 @@ def test_errors_of_rising_maxima_do_not_add_up_along_a_row(step):
     check(np.floor(np.arange(V) / 4096) * step, torch.float32, 513)
     far = np.arange(V) / V * 300.0                         # references are left behind many times over
     check(far, torch.float32, 2)
+
+
+@pytest.mark.parametrize("G,W", [(1, 1), (300, 4), (2000, 7)])
+def test_running_scores_replaced_in_place(G, W):
+    V = 333
+    rng = np.random.default_rng(5)
+    z = torch.from_numpy(rng.normal(size=(G * W, V)).astype(np.float32)).cuda()
+    running = torch.from_numpy(rng.normal(size=(G, W)).astype(np.float32)).cuda()
+    a = pcb.beam(z, running, W, normalise=True)
+    ws = torch.empty(pcb.pc_beam_workspace_bytes(a), dtype=torch.uint8, device="cuda")
+    want = torch.empty((G, W), device="cuda"), torch.empty((G, W), dtype=torch.int32, device="cuda"), torch.empty((G, W), dtype=torch.int32, device="cuda")
+    got = running, torch.empty_like(want[1]), torch.empty_like(want[2])
+    pcb.pc_beam_select(a, ws, *want)
+    pcb.pc_beam_select(a, ws, *got)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))

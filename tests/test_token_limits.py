@@ -41,3 +41,22 @@ def test_log_probabilities_that_overlap_what_they_are_made_of_are_refused():
     for logp in (FAR, FAR + 4 * 10 * 32 * 4 - 4, FAR - 16 * 40 + 4, 2 * FAR, 2 * FAR + (127 * 64 + 16) * 4 - 4):
         assert status(pcb.lib().pc_predict(C.byref(m), FAR, 16, logp, 10, None, 0, None)) == "PC_ERR_ARG", logp
         assert "overlap" in (pcb.lib().pc_last_error() or b"").decode()
+
+
+def select(out_scores=5 * FAR, parents=6 * FAR, tokens=7 * FAR, n_out=4, groups=3):
+    a = pcb.pc_beam(groups=groups, beams=4, n_cats=50, n_out=n_out, scores=FAR, scores_type=1, scores_ld=60, normalise=0, running=2 * FAR, done=3 * FAR, done_token=0)
+    st = status(pcb.lib().pc_beam_select(C.byref(a), 4 * FAR, 1 << 20, out_scores, parents, tokens, None))
+    return st, (pcb.lib().pc_last_error() or b"").decode()
+
+
+def test_survivors_that_overlap_what_they_are_chosen_from_are_refused():
+    """A group's survivors are written while other groups still read; running scores may be replaced where a group has as many survivors as beams."""
+    last = ((3 * 4 - 1) * 60 + 50) * 2 - 4                 # scores; 3 x 4 running scores; 3 x 4 marks
+    for at in (FAR, FAR + last, 2 * FAR + 44, 2 * FAR - 44, 3 * FAR + 8, 3 * FAR - 44):
+        for what in ("out_scores", "parents", "tokens"):
+            st, message = select(**{what: at})
+            assert st == "PC_ERR_ARG" and "overlap" in message, (what, at)
+    for change in (dict(out_scores=2 * FAR, n_out=5), dict(out_scores=2 * FAR, n_out=3), dict(parents=2 * FAR), dict(tokens=2 * FAR), dict(tokens=6 * FAR), dict(parents=5 * FAR + 44),
+                   dict(out_scores=2 * FAR, parents=2 * FAR)):
+        st, message = select(**change)
+        assert st == "PC_ERR_ARG" and "overlap" in message, change
