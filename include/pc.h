@@ -246,7 +246,7 @@ enum { PC_F32 = 0, PC_BF16 = 1, PC_F16 = 2 };   /* element types of rows of logi
 /* Input nodes of one variable with their weights in each sample: n_blocks blocks of K nodes; block j's weights are the rows
  * rows[j] .. rows[j] + K - 1 of `weights` (samples contiguous, `stride` floats between rows, stride >= B), its categorical
  * table is tables[table[j]].  rows / table are device arrays of n_blocks entries, or NULL: rows[j] = j * K, table[j] = j.  A
- * block whose rows or table lie outside [0, n_rows) / [0, n_tables) is left out.  K: 1 .. 128, n_rows >= K.  Weights and table
+ * block whose rows or table lie outside [0, n_rows) / [0, n_tables) is left out.  K: 1 .. 128, n_rows >= K, n_cats <= 2^29 - 32.  Weights and table
  * entries are not negative and at most 2^20 (probabilities).  Tables are 16-byte aligned; samples behind B are not used. */
 typedef struct {
     int32_t K, n_blocks, n_cats, n_tables;

@@ -958,7 +958,7 @@ static pc_status check_mixture(const pc_mixture *m, int32_t B)
     if (m->n_rows < m->K) return fail(PC_ERR_ARG, "weights have fewer rows than a block");
     if (m->stride < B) return fail(PC_ERR_ARG, "stride is smaller than B");
     if ((int64_t)m->n_blocks * m->K > 1 << 30) return fail(PC_ERR_TOO_LARGE, "more than 2^30 states");
-    if (m->n_cats > 1 << 29) return fail(PC_ERR_TOO_LARGE, "more than 2^29 categories");        // a grid has fewer than 2^32 threads along x
+    if (m->n_cats > (1 << 29) - 32) return fail(PC_ERR_TOO_LARGE, "more than 2^29 - 32 categories");   // a grid has fewer than 2^32 threads along x, 256 for 32 categories
     if (!m->rows && (int64_t)m->n_blocks * m->K > m->n_rows) return fail(PC_ERR_ARG, "weights have fewer than n_blocks * K rows");
     if (!m->table && m->n_blocks > m->n_tables) return fail(PC_ERR_ARG, "fewer tables than blocks");
     if (!aligned_to(m->weights, 4) || !aligned_to(m->rows, 4) || !aligned_to(m->table, 4))

@@ -60,3 +60,11 @@ def test_survivors_that_overlap_what_they_are_chosen_from_are_refused():
                    dict(out_scores=2 * FAR, parents=2 * FAR)):
         st, message = select(**change)
         assert st == "PC_ERR_ARG" and "overlap" in message, change
+
+
+@pytest.mark.parametrize("n_cats,want", [((1 << 29) - 32, "PC_OK"), ((1 << 29) - 31, "PC_ERR_TOO_LARGE"), (1 << 29, "PC_ERR_TOO_LARGE")])
+def test_categories_whose_grid_has_too_many_threads_are_refused(n_cats, want):
+    """A workgroup of 256 threads for every 32 categories: 2^24 of them would be 2^32 threads."""
+    m, n = pcb.pc_mixture(K=32, n_blocks=1, n_cats=n_cats, n_tables=1, n_rows=32, stride=64, weights=P, rows=None, table=None), C.c_size_t()
+    assert ((n_cats + 31) // 32 * 256 < 1 << 32) == (want == "PC_OK")
+    assert status(pcb.lib().pc_predict_workspace_bytes(C.byref(m), 3, C.byref(n))) == want
