@@ -305,7 +305,7 @@ typedef struct {
 } pc_distill;
 pc_status pc_distill_workspace_bytes(const pc_distill *d, size_t *bytes);
 /* loss: device fp32 [rows]; stats: device fp32 [rows][2], the row's maximum m and log sum exp((student - m) / T) (zeros where
- * `normalised`), for pc_distill_backward.  workspace: 16-byte aligned. */
+ * `normalised`), for pc_distill_backward.  workspace: reserved; pc_distill_workspace_bytes says 0, the call reads neither and takes NULL. */
 pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t workspace_bytes, float *loss, float *stats, void *stream);
 /* dstudent[r][c] = scale * dloss[r] * gradient, rounded once to the student's type; dloss: device fp32 [rows] or NULL (ones);
  * dstudent_ld >= n_cats elements between rows; dstudent may be the student's rows themselves (same ld).  Rows whose scale * dloss is 0

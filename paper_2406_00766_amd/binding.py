@@ -589,7 +589,7 @@ def _array(name, t, dtype, shape, index):
 
 
 def pc_distill_forward(d: distill, workspace, loss, stats, stream=None):
-    """loss float32 [rows], stats float32 [rows, 2]."""
+    """loss float32 [rows], stats float32 [rows, 2].  workspace: None (none is needed)."""
     import torch
     _call(d.index, stream, lib().pc_distill_forward, C.byref(d.struct), *_workspace(workspace, d.index),
           _array("loss", loss, torch.float32, (d.rows,), d.index), _array("stats", stats, torch.float32, (d.rows, 2), d.index))

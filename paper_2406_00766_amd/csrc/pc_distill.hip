@@ -389,17 +389,12 @@ pc_status pc_distill_workspace_bytes(const pc_distill *d, size_t *bytes)
     return PC_OK;
 }
 
-pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t workspace_bytes, float *loss, float *stats, void *stream)
+pc_status pc_distill_forward(const pc_distill *d, void *, size_t, float *loss, float *stats, void *stream)
 {
     const pc_status st = check_distill(d);
     if (st != PC_OK || d->rows == 0) return st;
     if (!loss || !stats) return fail(PC_ERR_ARG, "NULL argument");
     if (!aligned_to(loss, 4) || !aligned_to(stats, 4)) return fail(PC_ERR_ARG, "loss and stats must be 4-byte aligned");
-    size_t need = 0;
-    pc_distill_workspace_bytes(d, &need);
-    if (need && !workspace) return fail(PC_ERR_ARG, "NULL argument");
-    if (workspace_bytes < need) return fail(PC_ERR_WORKSPACE, "workspace smaller than pc_distill_workspace_bytes");
-    if (need && !aligned_to(workspace, 16)) return fail(PC_ERR_ARG, "the workspace must be 16-byte aligned");
     const DistillDev dev = distill_dev(d);
     with_type(d->student_type, [&](auto s) {
         with_type(d->teacher_type, [&](auto t) {

@@ -58,8 +58,6 @@ __device__ inline void unpack_f32(const Pack<T> &r, float (&x)[Pack<T>::N])
         else if constexpr (std::is_same<T, f16_t>::value) x[i] = to_f32(r.v[i]);
         else x[i] = __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
 }
-template <typename T>
-__device__ inline void store_pack(T *p, const Pack<T> &v) { __builtin_memcpy(p, &v, 16); }
 typedef float pc_float2 __attribute__((ext_vector_type(2)));
 typedef __bf16 pc_bf16x2 __attribute__((ext_vector_type(2)));
 template <typename T>

@@ -68,3 +68,13 @@ def test_categories_whose_grid_has_too_many_threads_are_refused(n_cats, want):
     m, n = pcb.pc_mixture(K=32, n_blocks=1, n_cats=n_cats, n_tables=1, n_rows=32, stride=64, weights=P, rows=None, table=None), C.c_size_t()
     assert ((n_cats + 31) // 32 * 256 < 1 << 32) == (want == "PC_OK")
     assert status(pcb.lib().pc_predict_workspace_bytes(C.byref(m), 3, C.byref(n))) == want
+
+
+def test_distillation_takes_no_workspace():
+    """The query says 0 for every shape, and a call turns nothing down for its workspace: what it refuses here is the loss that is not there."""
+    for change in (dict(), dict(rows=1, n_cats=200000, student_ld=200000), dict(rows=100000), dict(top=1000, ids_ld=1000, teacher_ld=1000)):
+        d, n = distill(**change), C.c_size_t(99)
+        assert status(pcb.lib().pc_distill_workspace_bytes(C.byref(d), C.byref(n))) == "PC_OK" and n.value == 0
+        for workspace, size in ((None, 0), (P + 1, 7)):
+            assert status(pcb.lib().pc_distill_forward(C.byref(d), workspace, size, None, P, None)) == "PC_ERR_ARG"
+            assert (pcb.lib().pc_last_error() or b"").decode() == "NULL argument"
