@@ -236,18 +236,19 @@ pc_status pc_em_step(pc_circuit *c, float *theta, float *tables, float *theta_fl
                      float step, float pseudocount, void *stream);
 
 /* ---- Token models over circuits: predicting a variable, distilling from a teacher, decoding with beams ----
- * None of these calls needs a handle: their operands are what the descriptors name, which is read before the call
+ * None of these calls but pc_get_mixture needs a handle: their operands are what the descriptors name, which is read before the call
  * returns and not retained.  They run on the device the calling thread has current.  Like the passes they only
  * enqueue kernels on `stream` and may be captured; a call with no rows (groups) does nothing and returns PC_OK.
  * Workspaces (16-byte aligned; NULL where none is needed) are scratch of one call: nothing in them is kept from call to call, calls
- * that overlap in time need one each.  Results do not depend on what a workspace holds, and are the same on every run. */
+ * that overlap in time need one each.  Their bytes are those of the call that is asked about; a smaller batch may need more than a larger one.
+ * Results do not depend on what a workspace holds, and are the same on every run. */
 enum { PC_F32 = 0, PC_BF16 = 1, PC_F16 = 2 };   /* element types of rows of logits */
 
 /* Input nodes of one variable with their weights in each sample: n_blocks blocks of K nodes; block j's weights are the rows
  * rows[j] .. rows[j] + K - 1 of `weights` (samples contiguous, `stride` floats between rows, stride >= B), its categorical
  * table is tables[table[j]].  rows / table are device arrays of n_blocks entries, or NULL: rows[j] = j * K, table[j] = j.  A
- * block whose rows or table lie outside [0, n_rows) / [0, n_tables) is left out.  K: 1 .. 128, n_rows >= K, n_cats <= 2^29 - 32.  Weights and table
- * entries are not negative and at most 2^20 (probabilities).  Tables are 16-byte aligned; samples behind B are not used. */
+ * block whose rows or table lie outside [0, n_rows) / [0, n_tables) is left out.  K: 1 .. 128, n_rows >= K, n_cats <= 2^29 - 32.
+ * Weights and table entries are not negative and at most 2^20 (probabilities).  Tables are 16-byte aligned; samples behind B are not used. */
 typedef struct {
     int32_t K, n_blocks, n_cats, n_tables;
     int64_t n_rows, stride;
@@ -263,8 +264,8 @@ pc_status pc_get_mixture(const pc_circuit *c, int32_t var, int32_t B, const void
                          pc_mixture *out);
 
 /* Predictive distribution:  logp[b][c] = log sum_j sum_k weights[rows[j] + k][b] * tables[table[j]][c][k],  b < B, c < n_cats,
- * ld >= n_cats floats between the rows of logp, which overlaps neither tables nor weights.  A probability below FLT_MIN (a sample without weights: all of them) gives
- * -inf.  Sums are kept in fp32, products are off by at most 2^-22 of themselves, whatever batch a sample is in. */
+ * ld >= n_cats floats between the rows of logp, which overlaps neither tables nor weights (PC_ERR_ARG).  A probability below FLT_MIN (a sample
+ * without weights: all of them) gives -inf.  Sums are kept in fp32, products are off by at most 2^-22 of themselves, whatever batch a sample is in. */
 pc_status pc_predict_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float *logp, int64_t ld, void *workspace,
                      size_t workspace_bytes, void *stream);
@@ -275,8 +276,9 @@ pc_status pc_predict(const pc_mixture *m, const float *tables, int32_t B, float 
  * which is the objective's gradient with respect to log tables[t][c][k];  table_flow = scale * flow for the tables that the mixture
  * names, added to what is there where `accumulate` is set.  With dlogp = -q (a loss -sum q logp, q >= 0) and scale = -1 these are
  * the flows of an EM step on soft targets, ready for pc_em_step.  Entries of logp below log FLT_MIN add nothing.  Sums are kept in
- * fp32, products weights * dlogp / exp(logp) are off by at most 2^-22 of themselves (by 2^-102 of the weight where that is more).  table_flow is 16-byte aligned, laid out like the tables, and
- * overlaps neither them nor the weights, logp or dlogp (PC_ERR_ARG); flows of tables that no block names stay as they are. */
+ * fp32, products weights * dlogp / exp(logp) are off by at most 2^-22 of themselves (by 2^-102 of the weight where that is more).
+ * table_flow is 16-byte aligned, laid out like the tables, and overlaps neither them nor the weights, logp or dlogp (PC_ERR_ARG); flows of
+ * tables that no block names stay as they are. */
 pc_status pc_predict_backward_workspace_bytes(const pc_mixture *m, int32_t B, size_t *bytes);
 pc_status pc_predict_backward(const pc_mixture *m, const float *tables, int32_t B, const float *logp, int64_t logp_ld,
                               const float *dlogp, int64_t dlogp_ld, float scale, int32_t accumulate, float *table_flow,
@@ -308,14 +310,15 @@ pc_status pc_distill_workspace_bytes(const pc_distill *d, size_t *bytes);
  * `normalised`), for pc_distill_backward.  workspace: reserved; pc_distill_workspace_bytes says 0, the call reads neither and takes NULL. */
 pc_status pc_distill_forward(const pc_distill *d, void *workspace, size_t workspace_bytes, float *loss, float *stats, void *stream);
 /* dstudent[r][c] = scale * dloss[r] * gradient, rounded once to the student's type; dloss: device fp32 [rows] or NULL (ones);
- * dstudent_ld >= n_cats elements between rows; dstudent may be the student's rows themselves (same ld).  Rows whose scale * dloss is 0
+ * dstudent_ld >= n_cats elements between rows; dstudent may be the student's rows themselves (same ld), else it does not overlap them (PC_ERR_ARG).  Rows whose scale * dloss is 0
  * get 0 whatever they hold. */
 pc_status pc_distill_backward(const pc_distill *d, const float *stats, const float *dloss, float scale, void *dstudent,
                               int64_t dstudent_ld, void *stream);
 
 /* Beam search: of all beams and categories of a group the n_out best.  Candidate (beam, c) has the score
- * running[beam] + z, z = scores[beam][c], minus log sum_c' exp(scores[beam][c']) where `normalise` (rows of logits), added in 64 bits.  The exponentials
- * are fp32, their sum over a row and its logarithm 64 bits: it is off by at most 2^-17 (1e-7 for 50257 normal logits), and beams whose scores lie closer may change places.
+ * running[beam] + z, z = scores[beam][c], minus log sum_c' exp(scores[beam][c']) where `normalise` (rows of logits), added in 64 bits.
+ * The exponentials are fp32, their sum over a row and its logarithm 64 bits: the logarithm is off by at most 2^-17 (1e-7 for 50257 normal
+ * logits), and candidates of different beams whose scores lie closer may change places.
  * A finished beam (done != 0) has the one candidate done_token with z = 0; its row is not read.  Order: higher score, then lower
  * beam, then (within a beam) higher z, then lower category.  Candidates that are no numbers or whose beam's running score is
  * no number below +inf count as -inf, as do all of a row whose log-normaliser is no finite number; candidates of -inf come last, by
@@ -331,13 +334,13 @@ typedef struct {
     int32_t done_token;
 } pc_beam;
 pc_status pc_beam_workspace_bytes(const pc_beam *a, size_t *bytes);
-/* out_scores (fp32), parents (beam within the group), tokens: device, [groups][n_out], best first.  workspace: 16-byte aligned.  Outputs overlap neither
- * each other nor scores, running or done (PC_ERR_ARG), but out_scores may be `running` where n_out == beams. */
+/* out_scores (fp32), parents (beam within the group), tokens: device, [groups][n_out], best first.  workspace: 16-byte aligned.
+ * Outputs overlap neither each other nor scores, running or done (PC_ERR_ARG), but out_scores may be `running` where n_out == beams. */
 pc_status pc_beam_select(const pc_beam *a, void *workspace, size_t workspace_bytes, float *out_scores, int32_t *parents,
                          int32_t *tokens, void *stream);
 /* What each survivor takes along: row g * n_out + i of dst = row g * beams + parents[g][i] of src, for up to PC_MAX_STATES arrays
  * of rows in one launch (evidence rows x and mask, hidden states, caches).  Strides are in bytes; a row's bytes behind row_bytes
- * are not touched.  dst must not overlap any src or other dst (PC_ERR_ARG).  A parent outside [0, beams) leaves its row of dst as it was. */
+ * are not touched.  dst, from its first row to its last, must not overlap any src or other dst (PC_ERR_ARG).  A parent outside [0, beams) leaves its row of dst as it was. */
 #define PC_MAX_STATES 16
 typedef struct {
     const void *src;

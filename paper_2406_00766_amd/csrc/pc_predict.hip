@@ -109,9 +109,9 @@ __device__ inline floatx16 mfma(const uint4 &a, const uint4 &b, const floatx16 &
 // stages the weights [states][samples] into LDS as planes in operand order.  While a chunk is multiplied the next one is split and staged
 // and the one after it is on its way; one barrier a chunk.
 // The samples are the instruction's rows, so that a store covers 32 neighbouring categories.  Bound by reading the tables and splitting them up to some
-// 64 samples (4096 states x 50257: B = 16 221 us, 3.7 TB/s; B = 64 249), then by the matrix cores (B = 128 341 us; B = 256 590: 1070 TFLOP/s of
-// bf16 products, six to a product; a large bf16 product reaches 1130).
-// Waves of 128 samples and more (READY) find the weights' planes ready: every workgroup splitting them anew took 382 us at B = 128, 624 at B = 256.
+// 64 samples (4096 states x 50257: B = 16 215 us, 3.8 TB/s; B = 64 238), then by the matrix cores (B = 128 331 us; B = 256 545: 1160 TFLOP/s of
+// bf16 products, six to a product; a large bf16 product reaches 1450.  Both once the clock has settled: of a row of calls the first 30 take up to 770).
+// Waves of 128 samples and more (READY) find the weights' planes ready: every workgroup splitting them anew took 364 us at B = 128, 569 at B = 256.
 // A workgroup adds up `len` states from blockIdx.z * len on; several parts: the sums go to `sums` and k_predict_join takes the logarithm.
 // Where a group of four states begins in the tables and in the weights is looked up in LDS, a window of states at a time, so that
 // blocks need not be as long as a chunk; WHOLE: they are multiples of KC, one look-up serves a wave's part.
@@ -555,9 +555,9 @@ __global__ __launch_bounds__(64 * kPrepareWaves) void k_flow_prepare(const pc_mi
 // Table flows.  A workgroup of 2 x 2 waves owns a tile of 64 I categories x 64 I columns, a column being a node of a block.  The samples are
 // added up 16 at a time from planes in LDS: g / p of the tile's categories and the weights of its columns, three planes each, six
 // products (the terms of a flow have either sign and are few, so that nothing averages out; the fp32 matrix instructions took longer:
-// 4096 states x 50257, B = 256, gradients without zeros 1372 us).  While a step is multiplied the next one's operands are staged and the one
-// after is on its way.  Bound by the matrix cores' sustained rate from some 100 samples on (B = 256: 795 us, six products alone 557; making the
-// planes in every tile took 1010), before by reading the tables and writing their flows (B = 32: 358 us, 4.7 TB/s), which the products of a
+// 4096 states x 50257, B = 256, gradients without zeros 1372 us against 795).  While a step is multiplied the next one's operands are staged and the one
+// after is on its way.  Bound by the matrix cores' sustained rate from some 100 samples on (B = 256: 742 us in a long row of calls, six products at
+// the rate of a large one 436; making the planes in every tile took a quarter more), before by reading the tables and writing their flows (B = 32: 346 us, 4.9 TB/s), which the products of a
 // CU's other workgroups cover.
 // MARKED: operands as k_flow_prepare has left them.  Of a segment whose samples mostly have no gradient among the tile's categories (targets of
 // a few categories a sample: an EM step) only those that do are added up, their g / p made here and their weights taken by sample,
@@ -842,14 +842,14 @@ __global__ __launch_bounds__(256) void k_flow_join(const pc_mixture m, const flo
 static int64_t one_rows(const pc_mixture &m) { return 64 / ((m.K + 3) / 4) * kOneRows; }      // categories of a wave of k_predict_one
 
 // How a prediction is launched.
-// One sample of many categories: no matrix cores (100 states x 20 blocks x 50257 78 us against 123, 32 states x 8 18 against 31; 4096 states 146 and
-// 246, 8192 states x 20000 127 and 229), where that makes waves enough for two to a CU.
+// One sample of many categories: no matrix cores (100 states x 20 blocks x 50257 72 us against 116, 32 states x 8 12 against 25; 4096 states 139 and
+// 229, 8192 states x 20000 120 and 220), where that makes waves enough for two to a CU.
 // Samples a wave: as many of 256 as there are, so that the tables are read once; 128 below 4096 categories (256 and 128: 4096 states x 4000, B = 256
-// 78 us and 74, x 9000 128 and 139, x 50257 590 and 690); 64 from 17 samples on (64 and 32: 4096 states x 50257, B = 24 235 us and 275, B = 16 237 and
-// 221); fewer where that leaves a SIMD without a wave (the tables of few categories stay in the caches).
+// 68 us and 64, x 9000 116 and 127, x 50257 545 and 645); 64 from 17 samples on (64 and 32: 4096 states x 50257, B = 24 229 us and 268, B = 16 231 and
+// 215); fewer where that leaves a SIMD without a wave (the tables of few categories stay in the caches).
 // Where there is less than a workgroup to a CU and the states are many (1024: an exchange and a second launch take some 4 us) they are dealt out
-// in parts of at least 256, as many as fill the GPU once, whose sums k_predict_join adds up (4096 states x 256, B = 256 24 us against 64;
-// x 5000 89 against 468; x 16000, 2048 states, B = 500 203 against 262; with more workgroups, 1024 states x 50257, B = 64 84 against 69).
+// in parts of at least 256, as many as fill the GPU once, whose sums k_predict_join adds up (4096 states x 256, B = 256 17 us against 57;
+// x 5000 80 against 470; x 16000, 2048 states, B = 500 181 against 251; with more workgroups, 1024 states x 50257, B = 64 74 against 58).
 struct PredictPlan { bool one; int32_t nt, len, parts, columns; size_t sums, bytes; };
 static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
 {
@@ -873,7 +873,7 @@ static PredictPlan predict_plan(const pc_mixture &m, int32_t B)
 }
 
 // Samples of a first launch with the widest waves, the others in a second one: where half of such a wave would do for those (4096 states
-// x 50257, B = 257 712 us against 1037, B = 384 947 against 1089).
+// x 50257, B = 257 665 us against 1004, B = 384 876 against 1042).
 static int32_t predict_first(const pc_mixture &m, int32_t B)
 {
     if (B <= 256 || B % 256 == 0 || B % 256 > 128) return B;
